@@ -221,6 +221,42 @@ xenos_status xenos_run_chain(xenos_plan* plan, int chain, const void* d_input, v
 xenos_status xenos_probe_mfma(const xenos_hw_info* hw, void* d_out, size_t out_bytes, int iters, int data, void* hip_stream, double* flops);
 xenos_status xenos_probe_read(const xenos_hw_info* hw, const void* d_in, size_t bytes, void* d_out, size_t out_bytes, void* hip_stream);
 
+/* ---- Operators of a token model's serving step ---------------------------------------------------------------------------
+ * The matrix products, the cache and the attention between them, and what is read from the logits, for programs that
+ * serve the transformer workloads (Section 7.1) beside the CNN graphs.  Called one by one on device buffers, without a plan: every pointer below
+ * is a DEVICE pointer (descriptors themselves are host structs, borrowed for the call), every call is asynchronous on
+ * hip_stream, allocates nothing and keeps nothing.  Sizes of zero are allowed and do nothing.  Forward passes only. */
+
+/* Rows in 8-bit integers.  q[r][i] = rint(x[r][i] g[i] * (127 / a)) with a = max(2^-100, max_i |x[r][i] g[i]|), rounded to nearest even;
+ * d_scale[r] = a / 127, so that q * scale stands for x g.  d_gamma (fp32, may be NULL: g = 1 and no norm) are the weights of an RMS norm in front:
+ * the scale then also holds the row's factor 1 / sqrt(mean x^2 + eps).  A row that holds a NaN or an infinity stands for NaN.
+ * The tokens' activations take this form on every call, a layer's weights ([out_c][cols], one scale per output channel) once.
+ * x: `rows` rows of `cols` elements, row_stride elements apart.  q: rows XENOS_QUANT_PITCH(cols) bytes apart, zeros behind
+ * the row's own values, 16-byte aligned.  cols is at most XENOS_QUANT_MAX_COLS (the sums of a product stay within 32 bits). */
+#define XENOS_QUANT_MAX_COLS 131072
+#define XENOS_QUANT_PITCH(cols) (((long long)(cols) + 127) / 128 * 128)
+xenos_status xenos_quant_rows(const void* d_x, xenos_dtype dtype, int rows, int cols, long long row_stride, const float* d_gamma, float eps,
+                              void* d_q, float* d_scale, void* hip_stream);
+
+/* Product of two such matrices: out[m][n] = act(scale[m] * w_scale[n] * sum_k q[m][k] w[n][k] + bias[n] + residual[m][n]).
+ * The sum is a whole number, exact; the rest is fp32, rounded once to `dtype`.  q and w: XENOS_QUANT_PITCH(cols) bytes a row, 16-byte aligned, zeros behind
+ * column `cols`; weights lie in -127 .. 127.  residual (of `dtype`, may be NULL; may be out itself) and bias (may be NULL) as in the linked chains: added before the ReLU. */
+typedef struct {
+  int rows, cols, out_c;
+  const void* d_q;
+  const float* d_scale;
+  const void* d_w;
+  const float* d_w_scale;
+  const float* d_bias;
+  const void* d_residual;
+  long long residual_stride;    /* elements from one row to the next */
+  int relu;
+  xenos_dtype dtype;            /* of residual and out */
+  void* d_out;
+  long long out_stride;
+} xenos_quant_matmul_args;
+xenos_status xenos_quant_matmul(const xenos_quant_matmul_args* args, void* hip_stream);
+
 /* Releases a graph or a plan (either handle type; NULL is ignored).  A plan holds a reference to
  * nothing of the graph after xenos_plan_link_split returns. */
 void xenos_destroy(void* graph_or_plan);

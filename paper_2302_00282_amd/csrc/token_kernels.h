@@ -1,0 +1,36 @@
+// Arguments and launchers of the kernels of a token model's serving step (8-bit linear layers, quantised cache, attention,
+// log probabilities).  The entry points in xenos_tokens.cpp have checked everything that is said here of sizes and alignment.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+namespace xenos {
+
+constexpr float kTinyAmplitude = 7.888609052210118e-31f;     // 2^-100: 127 / it is finite, and so is every quantised row
+constexpr int kQuantPitch = 128;                             // bytes: a quantised row's own, rounded up, zeros behind them
+inline long long quant_pitch(long long cols) { return (cols + kQuantPitch - 1) / kQuantPitch * kQuantPitch; }
+
+struct QuantRowsArgs {
+  const void* x;                                             // [rows][stride], `cols` of each row
+  const float* gamma;                                        // [cols] or null
+  int8_t* q;                                                 // [rows][pitch]
+  float* scale;                                              // [rows]
+  long long stride, pitch;
+  int rows, cols;
+  float eps;
+};
+int launch_quant_rows(const QuantRowsArgs& a, int dtype, void* stream);
+
+struct QuantMatmulArgs {
+  const int8_t *x, *w;                                       // [M][pitch], [N][pitch]: K bytes and zeros
+  const float *xs, *ws, *bias;                               // [M], [N], [N] or null
+  const void* res;                                           // [M][res_stride] or null, of out's type
+  void* out;                                                 // [M][out_stride]
+  long long pitch, res_stride, out_stride;
+  int M, N;
+  int relu;
+  int vec_out;                                               // rows of out and res start at multiples of four elements, whole fours are stored at once
+};
+int launch_quant_matmul(const QuantMatmulArgs& a, int dtype, void* stream);
+
+}  // namespace xenos

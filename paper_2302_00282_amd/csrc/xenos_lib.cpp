@@ -19,14 +19,15 @@
 
 #include "../../include/xenos.h"
 #include "kernels.h"
+#include "status.h"
 
 using namespace xenos;
 
 namespace {
-
 thread_local std::string g_err;
+}
 
-xenos_status fail(xenos_status st, const char* fmt, ...) {
+xenos_status xenos::fail(xenos_status st, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -35,6 +36,8 @@ xenos_status fail(xenos_status st, const char* fmt, ...) {
   g_err = buf;
   return st;
 }
+
+namespace {
 
 constexpr uint32_t MAGIC_GRAPH = 0x58474631u, MAGIC_PLAN = 0x58504c31u;
 

@@ -1,0 +1,60 @@
+// C-ABI entry points of the operators of a token model's serving step: what a caller hands over is checked here, then launched.
+#include <algorithm>
+#include <hip/hip_runtime.h>
+
+#include "status.h"
+#include "token_kernels.h"
+
+using namespace xenos;
+
+namespace {
+
+// The launch geometry has fewer than 2^32 threads.
+constexpr long long kMostGroups = 1ll << 22;
+
+bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
+size_t size_of(xenos_dtype t) { return t == XENOS_BF16 ? 2 : 4; }
+bool known(xenos_dtype t) { return t == XENOS_F32 || t == XENOS_BF16; }
+
+xenos_status launched(int err, const char* what) {
+  return err ? fail(XENOS_EDEVICE, "%s: %s", what, hipGetErrorString((hipError_t)err)) : XENOS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+xenos_status xenos_quant_rows(const void* d_x, xenos_dtype dtype, int rows, int cols, long long row_stride, const float* d_gamma, float eps,
+                              void* d_q, float* d_scale, void* hip_stream) {
+  if (rows < 0 || cols <= 0 || !known(dtype)) return fail(XENOS_EINVAL, "xenos_quant_rows: %d rows of %d columns, type %d", rows, cols, (int)dtype);
+  if (cols > XENOS_QUANT_MAX_COLS) return fail(XENOS_EUNSUPPORTED, "xenos_quant_rows: %d columns, at most %d", cols, XENOS_QUANT_MAX_COLS);
+  if (rows == 0) return XENOS_OK;
+  if (!d_x || !d_q || !d_scale) return fail(XENOS_EINVAL, "xenos_quant_rows: NULL argument");
+  if (rows > 1 && row_stride < cols) return fail(XENOS_ESHAPE, "xenos_quant_rows: rows of %d elements, %lld apart", cols, row_stride);
+  if (!aligned(d_x, size_of(dtype)) || !aligned(d_gamma, 4) || !aligned(d_q, 16) || !aligned(d_scale, 4))
+    return fail(XENOS_EINVAL, "xenos_quant_rows: a buffer is not aligned (the quantised rows: to 16 bytes)");
+  if (d_gamma && !(eps >= 0.f)) return fail(XENOS_EINVAL, "xenos_quant_rows: eps %g", (double)eps);
+  QuantRowsArgs a{d_x, d_gamma, (int8_t*)d_q, d_scale, rows > 1 ? row_stride : 0, quant_pitch(cols), rows, cols, eps};
+  return launched(launch_quant_rows(a, dtype, hip_stream), "xenos_quant_rows");
+}
+
+xenos_status xenos_quant_matmul(const xenos_quant_matmul_args* p, void* hip_stream) {
+  if (!p || p->rows < 0 || p->cols <= 0 || p->out_c < 0 || !known(p->dtype)) return fail(XENOS_EINVAL, "xenos_quant_matmul: bad argument");
+  if (p->cols > XENOS_QUANT_MAX_COLS) return fail(XENOS_EUNSUPPORTED, "xenos_quant_matmul: %d columns, at most %d", p->cols, XENOS_QUANT_MAX_COLS);
+  if (p->rows == 0 || p->out_c == 0) return XENOS_OK;
+  if (!p->d_q || !p->d_scale || !p->d_w || !p->d_w_scale || !p->d_out) return fail(XENOS_EINVAL, "xenos_quant_matmul: NULL argument");
+  if (p->rows > 1 && (p->out_stride < p->out_c || (p->d_residual && p->residual_stride < p->out_c)))
+    return fail(XENOS_ESHAPE, "xenos_quant_matmul: rows of %d elements, %lld (out) and %lld (residual) apart", p->out_c, p->out_stride, p->residual_stride);
+  const size_t esz = size_of(p->dtype);
+  if (!aligned(p->d_q, 16) || !aligned(p->d_w, 16) || !aligned(p->d_scale, 4) || !aligned(p->d_w_scale, 4) || !aligned(p->d_bias, 4) || !aligned(p->d_out, esz) ||
+      !aligned(p->d_residual, esz))
+    return fail(XENOS_EINVAL, "xenos_quant_matmul: a buffer is not aligned (quantised rows: to 16 bytes)");
+  if (((p->rows + 63ll) / 64) * ((p->out_c + 15ll) / 16) > kMostGroups)
+    return fail(XENOS_EUNSUPPORTED, "xenos_quant_matmul: %d x %d results are more than one launch holds", p->rows, p->out_c);
+  QuantMatmulArgs a{(const int8_t*)p->d_q, (const int8_t*)p->d_w, p->d_scale, p->d_w_scale, p->d_bias, p->d_residual, p->d_out, quant_pitch(p->cols),
+                    p->rows > 1 ? p->residual_stride : 0, p->rows > 1 ? p->out_stride : 0, p->rows, p->out_c, p->relu ? 1 : 0, 0};
+  a.vec_out = a.out_stride % 4 == 0 && aligned(a.out, 4 * esz) && (!a.res || (a.res_stride % 4 == 0 && aligned(a.res, 4 * esz)));
+  return launched(launch_quant_matmul(a, p->dtype, hip_stream), "xenos_quant_matmul");
+}
+
+}  // extern "C"

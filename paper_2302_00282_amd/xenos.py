@@ -54,6 +54,12 @@ class PlanOpts(C.Structure):
     _fields_ = [("link", C.c_int), ("split", C.c_int), ("compute", C.c_int), ("tile", C.c_int)]
 
 
+class QuantMatmulArgs(C.Structure):
+    _fields_ = [("rows", C.c_int), ("cols", C.c_int), ("out_c", C.c_int), ("d_q", C.c_void_p), ("d_scale", C.c_void_p),
+                ("d_w", C.c_void_p), ("d_w_scale", C.c_void_p), ("d_bias", C.c_void_p), ("d_residual", C.c_void_p), ("residual_stride", C.c_longlong),
+                ("relu", C.c_int), ("dtype", C.c_int), ("d_out", C.c_void_p), ("out_stride", C.c_longlong)]
+
+
 class XenosError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"xenos status {status}: {msg}")
@@ -89,12 +95,14 @@ def lib():
         L.xenos_plan_tune.argtypes = [vp, vp, vp, vp, C.c_int, C.POINTER(C.c_int)]
         L.xenos_probe_mfma.argtypes = [C.POINTER(HwInfo), vp, C.c_size_t, C.c_int, C.c_int, vp, C.POINTER(C.c_double)]
         L.xenos_probe_read.argtypes = [C.POINTER(HwInfo), vp, C.c_size_t, vp, C.c_size_t, vp]
+        L.xenos_quant_rows.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_longlong, vp, C.c_float, vp, vp, vp]
+        L.xenos_quant_matmul.argtypes = [C.POINTER(QuantMatmulArgs), vp]
         L.xenos_destroy.argtypes = [vp]
         L.xenos_destroy.restype = None
         L.xenos_last_error.restype = C.c_char_p
         for f in ("xenos_graph_create", "xenos_plan_link_split", "xenos_plan_query", "xenos_plan_bind",
                   "xenos_run", "xenos_run_graph", "xenos_run_static", "xenos_run_with", "xenos_run_chain", "xenos_plan_tune",
-                  "xenos_probe_mfma", "xenos_probe_read"):
+                  "xenos_probe_mfma", "xenos_probe_read", "xenos_quant_rows", "xenos_quant_matmul"):
             getattr(L, f).restype = C.c_int
         _lib = L
     return _lib
@@ -188,6 +196,14 @@ def xenos_probe_mfma(d_out: int, out_bytes: int, iters: int, stream: int = 0, hw
 def xenos_probe_read(d_in: int, nbytes: int, d_out: int, out_bytes: int, stream: int = 0, hw: Optional[dict] = None):
     hwi = HwInfo(**(hw or MI355X))
     _check(lib().xenos_probe_read(C.byref(hwi), d_in, nbytes, d_out, out_bytes, stream))
+
+
+def xenos_quant_rows(d_x: int, dtype: int, rows: int, cols: int, row_stride: int, d_gamma: int, eps: float, d_q: int, d_scale: int, stream: int = 0):
+    _check(lib().xenos_quant_rows(d_x, dtype, rows, cols, row_stride, d_gamma, eps, d_q, d_scale, stream))
+
+
+def xenos_quant_matmul(args: QuantMatmulArgs, stream: int = 0):
+    _check(lib().xenos_quant_matmul(C.byref(args), stream))
 
 
 def xenos_destroy(handle: Optional[int]):

@@ -1,0 +1,184 @@
+"""The 8-bit linear layer: rows quantised on the GPU and their product against the definition in 64 bits, and what is refused."""
+import pytest
+import torch
+
+from paper_2302_00282_amd import tokens as T
+from paper_2302_00282_amd import xenos as X
+
+U32, U16 = 2.0 ** -24, 2.0 ** -8          # half a step of fp32 and of bf16, relative
+
+
+def drawn(rows, cols, dtype, seed, spread=True):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, cols, generator=g)
+    if spread:
+        x *= torch.exp(2 * torch.randn(rows, 1, generator=g))
+    return x.to(dtype)
+
+
+def rows_by_definition(x, gamma=None, eps=1e-5):
+    """q by the formula's own fp32 operations (on the CPU), the scale in 64 bits."""
+    v = x.float() * gamma if gamma is not None else x.float()
+    a = v.abs().amax(-1, keepdim=True).clamp_min(2.0 ** -100)
+    q = torch.round(v * (torch.full_like(a, 127.0) / a))
+    scale = a.double() / 127
+    if gamma is not None:
+        scale = scale / torch.sqrt(x.double().square().mean(-1, keepdim=True) + eps)
+    return q, scale.squeeze(-1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 512), (3, 127), (2, 129), (5, 1001), (64, 4096), (2, 25088), (1, 131072), (70000, 8)])
+def test_quantized_rows(rows, cols, dtype, norm):
+    x = drawn(rows, cols, dtype, rows + cols)
+    gamma = torch.rand(cols, generator=torch.Generator().manual_seed(1)) - 0.3 if norm else None
+    q, scale = T.quantize_rows(x.cuda(), None if gamma is None else gamma.cuda())
+    want, want_scale = rows_by_definition(x, gamma)
+    assert q.shape == (rows, T.quant_pitch(cols)) and not q[:, cols:].any()
+    assert torch.equal(q[:, :cols].cpu().float(), want)
+    # one division; with a norm the sum of the squares (each lane's in order, then a tree: fewer than cols / 256 + 24 additions), a root and three more
+    steps = 1.01 if not norm else cols / 256 + 32
+    assert torch.all((scale.cpu().double() - want_scale).abs() <= steps * U32 * want_scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_quantized_rows_of_odd_strides_and_extreme_values(dtype):
+    wide = drawn(9, 1000, dtype, 3).cuda()
+    for view in (wide[:, 1:334], wide[::2, :333], wide[:, :333], wide.t()[:333].t(), wide[4:5, 3:]):
+        q, scale = T.quantize_rows(view)
+        want, want_scale = rows_by_definition(view.cpu())
+        assert torch.equal(q[:, :view.shape[1]].cpu().float(), want) and torch.all((scale.cpu().double() - want_scale).abs() <= 1.01 * U32 * want_scale)
+    x = drawn(6, 200, torch.float32, 4, False)
+    x[0] = 0
+    x[1] *= 1e-36                                              # (below the smallest amplitude: whole numbers of its own step)
+    x[2] *= 3e37
+    x[3, 7], x[4, 8], x[5, 9] = float("nan"), float("inf"), float("-inf")
+    q, scale = T.quantize_rows(x.to(dtype).cuda())
+    stands = q[:, :200].float() * scale[:, None]
+    want, want_scale = rows_by_definition(x.to(dtype))
+    assert torch.equal(q[:3, :200].cpu().float(), want[:3]) and not stands[0].any() and torch.isfinite(stands[:3]).all()
+    assert torch.isnan(stands[3:]).all()
+
+
+def product_by_definition(q, scale, w, w_scale, bias, residual, relu):
+    p = q.double() @ w.double().t() * scale.double()[:, None] * w_scale.double()
+    y, size = p, p.abs()
+    for t in (bias, residual):
+        if t is not None:
+            y, size = y + t.double(), size + t.double().abs()
+    return (y.clamp_min(0) if relu else y), size
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("extras", ["", "bias", "residual", "bias residual relu", "relu"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols,out_c", [(1, 1, 1), (1, 512, 2048), (2, 129, 17), (16, 640, 100), (17, 1000, 1003), (33, 128, 48), (64, 2560, 30), (65, 300, 130),
+                                             (127, 1001, 257), (128, 512, 128), (300, 257, 515), (513, 1536, 1000), (1, 40000, 64), (260, 25088, 40)])
+def test_product(rows, cols, out_c, dtype, extras):
+    q, scale = T.quantize_rows(drawn(rows, cols, dtype, 1).cuda())
+    w, w_scale = T.quantize_rows(drawn(out_c, cols, torch.float32, 2).cuda())
+    bias = drawn(1, out_c, torch.float32, 5)[0].cuda() if "bias" in extras else None
+    residual = drawn(rows, out_c, dtype, 6).cuda() if "residual" in extras else None
+    y = T.quant_matmul(q, scale, w, w_scale, cols, bias=bias, residual=residual, relu="relu" in extras, dtype=dtype)
+    want, size = product_by_definition(q, scale, w, w_scale, bias, residual, "relu" in extras)
+    # the sum as fp32, two scales, two sums: a step each; then the rounding to bf16
+    bound = 5.1 * U32 * size + (U16 * want.abs() if dtype == torch.bfloat16 else 0) + 1e-38
+    assert y.dtype == dtype and torch.all((y.double() - want).abs() <= bound)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,out_c", [(5, 1003), (5, 1000), (130, 257), (130, 256)])
+def test_residual_with_a_stride_and_in_place_order(rows, out_c, dtype):
+    cols = 257
+    x = drawn(rows, cols, dtype, 1).cuda()
+    w, w_scale = T.quantize_rows(drawn(out_c, cols, torch.float32, 2).cuda())
+    q, scale = T.quantize_rows(x)
+    for residual in (drawn(rows, out_c + 9, dtype, 3).cuda()[:, 3:3 + out_c], drawn(rows, out_c + 8, dtype, 3).cuda()[:, :out_c], drawn(out_c, rows, dtype, 3).cuda().t()):
+        y = T.linear(x, w, w_scale, residual=residual)
+        want, size = product_by_definition(q, scale, w, w_scale, None, residual, False)
+        assert torch.all((y.double() - want).abs() <= 5.1 * U32 * size + (U16 * want.abs() if dtype == torch.bfloat16 else 0))
+    # the residual's own memory as the result's (the C entry)
+    held = residual.contiguous()
+    a = X.QuantMatmulArgs(rows, cols, out_c, q.data_ptr(), scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), None, held.data_ptr(), out_c, 0,
+                          X.XENOS_BF16 if dtype == torch.bfloat16 else X.XENOS_F32, held.data_ptr(), out_c)
+    X.xenos_quant_matmul(a, torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(held, y)
+
+
+@pytest.mark.gpu
+def test_linear_of_more_dimensions_empty_ones_and_rows_without_numbers():
+    w, w_scale = T.quantize_rows(drawn(70, 96, torch.float32, 2).cuda())
+    x = drawn(6, 96, torch.bfloat16, 1).cuda()
+    gamma = torch.rand(96, device="cuda")
+    flat = T.linear(x, w, w_scale, gamma=gamma, residual=T.linear(x, w, w_scale))
+    assert torch.equal(T.linear(x.view(2, 3, 96), w, w_scale, gamma=gamma, residual=T.linear(x, w, w_scale).view(2, 3, 70)).view(6, 70), flat)
+    assert torch.equal(T.linear(x[0], w, w_scale), T.linear(x, w, w_scale)[0])
+    assert T.linear(x[:0], w, w_scale).shape == (0, 70) and T.linear(x, w[:0], w_scale[:0]).shape == (6, 0)
+    for rows in (6, 200):                                       # (both kernels)
+        x = drawn(rows, 96, torch.bfloat16, 1).cuda()
+        x[3, 5] = float("nan")
+        y = T.linear(x, w, w_scale, relu=True)
+        assert torch.isnan(y[3]).all() and torch.isfinite(y[torch.arange(rows) != 3]).all()
+
+
+@pytest.mark.gpu
+def test_linear_on_another_stream_follows_it():
+    w, w_scale = T.quantize_rows(drawn(512, 2048, torch.float32, 2).cuda())
+    x = drawn(64, 2048, torch.bfloat16, 1).cuda()
+    want = T.linear(x, w, w_scale)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        late = torch.zeros_like(x)
+        for _ in range(20):
+            late.add_(x, alpha=0.5).sub_(x, alpha=0.5)
+        late.add_(x)
+        y = T.linear(late, w, w_scale)
+    s.synchronize()
+    assert torch.equal(y, T.linear(late, w, w_scale)) and y.shape == want.shape
+
+
+@pytest.mark.gpu
+def test_linear_refuses():
+    w, w_scale = T.quantize_rows(drawn(16, 100, torch.float32, 2).cuda())
+    x = drawn(4, 100, torch.bfloat16, 1).cuda()
+    for call, status in [(lambda: T.linear(x.cpu(), w, w_scale), X.XENOS_EINVAL), (lambda: T.linear(x.half(), w, w_scale), X.XENOS_EUNSUPPORTED),
+                         (lambda: T.linear(x, w.float(), w_scale), X.XENOS_EINVAL), (lambda: T.linear(x[:, :99], w[:, :64], w_scale), X.XENOS_ESHAPE),
+                         (lambda: T.linear(x, w, w_scale[:3]), X.XENOS_ESHAPE), (lambda: T.linear(x, w, w_scale, bias=w_scale[:3]), X.XENOS_ESHAPE),
+                         (lambda: T.linear(x, w, w_scale, bias=w_scale.half()), X.XENOS_EINVAL), (lambda: T.linear(x, w, w_scale, residual=x), X.XENOS_ESHAPE),
+                         (lambda: T.linear(x, w, w_scale, gamma=w_scale), X.XENOS_ESHAPE), (lambda: T.linear(x.requires_grad_(), w, w_scale), X.XENOS_EUNSUPPORTED),
+                         (lambda: T.quantize_rows(x.detach()[:, :0]), X.XENOS_ESHAPE),
+                         (lambda: T.quantize_rows(torch.zeros(1, 131073, device="cuda")), X.XENOS_EUNSUPPORTED)]:
+        with pytest.raises(X.XenosError) as e:
+            call()
+        assert e.value.status == status, str(e.value)
+    with torch.no_grad():
+        assert T.linear(x, w, w_scale).shape == (4, 16)
+
+
+def test_c_entries_refuse_before_any_launch():
+    """On the host alone: nothing of this reaches a device."""
+    p = 256
+    rows = dict(d_x=p, dtype=0, rows=4, cols=100, row_stride=100, d_gamma=0, eps=1e-5, d_q=p, d_scale=p)
+    for change, status in [(dict(rows=-1), X.XENOS_EINVAL), (dict(cols=0), X.XENOS_EINVAL), (dict(dtype=2), X.XENOS_EINVAL), (dict(cols=131073, row_stride=1 << 20), X.XENOS_EUNSUPPORTED),
+                           (dict(d_x=0), X.XENOS_EINVAL), (dict(d_q=0), X.XENOS_EINVAL), (dict(d_scale=0), X.XENOS_EINVAL), (dict(row_stride=99), X.XENOS_ESHAPE),
+                           (dict(d_q=p + 8), X.XENOS_EINVAL), (dict(d_x=p + 2), X.XENOS_EINVAL), (dict(d_gamma=p + 1), X.XENOS_EINVAL), (dict(d_gamma=p, eps=-1.0), X.XENOS_EINVAL),
+                           (dict(d_gamma=p, eps=float("nan")), X.XENOS_EINVAL)]:
+        with pytest.raises(X.XenosError) as e:
+            X.xenos_quant_rows(**dict(rows, **change))
+        assert e.value.status == status and "xenos_quant_rows" in str(e.value)
+    X.xenos_quant_rows(**dict(rows, rows=0, d_x=0))
+    product = dict(rows=4, cols=100, out_c=8, d_q=p, d_scale=p, d_w=p, d_w_scale=p, d_bias=None, d_residual=None, residual_stride=0, relu=0, dtype=1, d_out=p, out_stride=8)
+    for change, status in [(dict(rows=-1), X.XENOS_EINVAL), (dict(cols=0), X.XENOS_EINVAL), (dict(out_c=-1), X.XENOS_EINVAL), (dict(dtype=7), X.XENOS_EINVAL),
+                           (dict(cols=1 << 20), X.XENOS_EUNSUPPORTED), (dict(d_w=None), X.XENOS_EINVAL), (dict(d_out=None), X.XENOS_EINVAL), (dict(d_w=p + 4), X.XENOS_EINVAL),
+                           (dict(d_out=p + 1), X.XENOS_EINVAL), (dict(d_bias=p + 2), X.XENOS_EINVAL), (dict(out_stride=7), X.XENOS_ESHAPE), (dict(d_residual=p, residual_stride=7), X.XENOS_ESHAPE),
+                           (dict(rows=1 << 30, out_c=1 << 30, out_stride=1 << 30), X.XENOS_EUNSUPPORTED)]:
+        with pytest.raises(X.XenosError) as e:
+            X.xenos_quant_matmul(X.QuantMatmulArgs(**dict(product, **change)))
+        assert e.value.status == status and "xenos_quant_matmul" in str(e.value)
+    X.xenos_quant_matmul(X.QuantMatmulArgs(**dict(product, rows=0, d_q=None)))
+    X.xenos_quant_matmul(X.QuantMatmulArgs(**dict(product, out_c=0, d_out=None)))
