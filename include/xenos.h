@@ -257,6 +257,28 @@ typedef struct {
 } xenos_quant_matmul_args;
 xenos_status xenos_quant_matmul(const xenos_quant_matmul_args* args, void* hip_stream);
 
+/* A cache of keys and values in 8-bit integers, quantised row by row (one token's head_dim values of one head) like xenos_quant_rows, in pages of
+ * page_tokens tokens that a caller deals out to its sequences in any order.  A token's slot is page * page_tokens + its place in the page.  Memory,
+ * all of it the caller's, in the order in which the attention's matrix instructions read it:
+ *   k       int8 [n_pages][heads][page_tokens][head_dim]
+ *   v       int8 [n_pages][heads][page_tokens / 16][head_dim][16]     (16 tokens of one dimension side by side)
+ *   scales  fp32 [n_pages][heads][page_tokens] each
+ * page_tokens: a multiple of 16; head_dim: a multiple of 16 up to 256; k and v 16-byte aligned.  Nothing has to be cleared: what no length
+ * names is not looked at, whatever bits it holds. */
+typedef struct {
+  int n_pages, page_tokens, heads, head_dim;
+  void *d_k, *d_v;
+  float *d_k_scale, *d_v_scale;
+} xenos_cache;
+
+/* Quantises and stores n_tokens rows of keys and values per head: element (t, h, d) of k lies at t * token_stride + h * head_stride + d.
+ * d_slots: n_tokens slots (64-bit), each used once; a slot below 0 or beyond the cache stores nothing. */
+xenos_status xenos_cache_write(const xenos_cache* cache, int n_tokens, const void* d_k, long long k_token_stride, long long k_head_stride,
+                               const void* d_v, long long v_token_stride, long long v_head_stride, xenos_dtype dtype, const long long* d_slots, void* hip_stream);
+
+/* The rows of n_tokens slots as the values they stand for, [n_tokens][heads][head_dim] of k and of v; a slot below 0 or beyond the cache reads zeros. */
+xenos_status xenos_cache_read(const xenos_cache* cache, int n_tokens, const long long* d_slots, void* d_k, void* d_v, xenos_dtype dtype, void* hip_stream);
+
 /* Releases a graph or a plan (either handle type; NULL is ignored).  A plan holds a reference to
  * nothing of the graph after xenos_plan_link_split returns. */
 void xenos_destroy(void* graph_or_plan);

@@ -33,4 +33,25 @@ struct QuantMatmulArgs {
 };
 int launch_quant_matmul(const QuantMatmulArgs& a, int dtype, void* stream);
 
+struct CacheArgs {
+  int8_t *k, *v;                                             // 16-byte aligned, the layouts of xenos.h
+  float *k_scale, *v_scale;
+  int n_pages, page, heads, dim;                             // page and dim are multiples of 16, dim <= 256
+};
+struct CacheWriteArgs {
+  CacheArgs c;
+  const void *k, *v;                                         // element (t, h, d) at t * token + h * head + d
+  long long k_token, k_head, v_token, v_head;
+  const long long* slots;
+  int tokens;
+};
+struct CacheReadArgs {
+  CacheArgs c;
+  const long long* slots;
+  void *k, *v;                                               // [tokens][heads][dim], 16-byte aligned
+  int tokens;
+};
+int launch_cache_write(const CacheWriteArgs& a, int dtype, void* stream);
+int launch_cache_read(const CacheReadArgs& a, int dtype, void* stream);
+
 }  // namespace xenos

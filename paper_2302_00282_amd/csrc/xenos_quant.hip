@@ -1,25 +1,8 @@
 // Rows in 8-bit integers with a scale each, and their product: the linear layers of a token model.
 #include "device_common.h"
-#include "token_kernels.h"
+#include "token_device.h"
 
 namespace xenos {
-
-typedef __attribute__((ext_vector_type(4))) int i32x4_t;
-
-// The largest |value| by its bits: a NaN's are above infinity's, so that it stays.
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
-
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v = umax(v, (uint32_t)__shfl_xor((int)v, o));
-  return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return v;
-}
 
 // Eight values of a row from element i on, those behind the row's end as zeros.
 template <typename T, bool VEC>
@@ -60,7 +43,7 @@ __global__ __launch_bounds__(1024) void quant_rows_kernel(QuantRowsArgs a) {
     __syncthreads();
     m = 0, sq = 0.f;
     for (int w = 0; w < waves; ++w) { m = umax(m, s_max[w]); sq += s_sum[w]; }
-    const float amp = __uint_as_float(umax(m, __float_as_uint(kTinyAmplitude))), inv = 127.f / amp;
+    const RowStep step8(m);
     for (int i = (int)threadIdx.x * 8; i < (int)a.pitch; i += step) {
       float f[8];
       load8<T, VEC>(row, i, a.cols, f);
@@ -68,11 +51,11 @@ __global__ __launch_bounds__(1024) void quant_rows_kernel(QuantRowsArgs a) {
   #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float v = a.gamma ? f[e] * (i + e < a.cols ? a.gamma[i + e] : 0.f) : f[e];
-        w[e >> 2] |= ((uint32_t)(int)rintf(v * inv) & 0xffu) << (8 * (e & 3));
+        w[e >> 2] |= ((uint32_t)step8(v) & 0xffu) << (8 * (e & 3));
       }
       *(uint2*)(q + i) = make_uint2(w[0], w[1]);
     }
-    if (threadIdx.x == 0) a.scale[at] = a.gamma ? amp / 127.f * (1.f / sqrtf(sq / (float)a.cols + a.eps)) : amp / 127.f;
+    if (threadIdx.x == 0) a.scale[at] = a.gamma ? step8.scale() * (1.f / sqrtf(sq / (float)a.cols + a.eps)) : step8.scale();
     __syncthreads();                                            // (s_max and s_sum are free again)
   }
 }

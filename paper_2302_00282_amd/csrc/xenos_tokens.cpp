@@ -20,6 +20,17 @@ xenos_status launched(int err, const char* what) {
   return err ? fail(XENOS_EDEVICE, "%s: %s", what, hipGetErrorString((hipError_t)err)) : XENOS_OK;
 }
 
+xenos_status cache_of(const xenos_cache* c, const char* who, CacheArgs& a) {
+  if (!c || c->n_pages < 0 || c->page_tokens <= 0 || c->heads <= 0 || c->head_dim <= 0) return fail(XENOS_EINVAL, "%s: bad cache description", who);
+  if (c->page_tokens % 16 || c->head_dim % 16 || c->head_dim > 256)
+    return fail(XENOS_EUNSUPPORTED, "%s: pages of %d tokens, heads of %d values (multiples of 16, at most 256 values)", who, c->page_tokens, c->head_dim);
+  if (c->n_pages > 0 && (!c->d_k || !c->d_v || !c->d_k_scale || !c->d_v_scale)) return fail(XENOS_EINVAL, "%s: NULL cache buffer", who);
+  if (!aligned(c->d_k, 16) || !aligned(c->d_v, 16) || !aligned(c->d_k_scale, 4) || !aligned(c->d_v_scale, 4))
+    return fail(XENOS_EINVAL, "%s: a cache buffer is not aligned (k and v: to 16 bytes)", who);
+  a = CacheArgs{(int8_t*)c->d_k, (int8_t*)c->d_v, c->d_k_scale, c->d_v_scale, c->n_pages, c->page_tokens, c->heads, c->head_dim};
+  return XENOS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -55,6 +66,34 @@ xenos_status xenos_quant_matmul(const xenos_quant_matmul_args* p, void* hip_stre
                     p->rows > 1 ? p->residual_stride : 0, p->rows > 1 ? p->out_stride : 0, p->rows, p->out_c, p->relu ? 1 : 0, 0};
   a.vec_out = a.out_stride % 4 == 0 && aligned(a.out, 4 * esz) && (!a.res || (a.res_stride % 4 == 0 && aligned(a.res, 4 * esz)));
   return launched(launch_quant_matmul(a, p->dtype, hip_stream), "xenos_quant_matmul");
+}
+
+xenos_status xenos_cache_write(const xenos_cache* cache, int n_tokens, const void* d_k, long long k_token_stride, long long k_head_stride,
+                               const void* d_v, long long v_token_stride, long long v_head_stride, xenos_dtype dtype, const long long* d_slots, void* hip_stream) {
+  CacheWriteArgs a{};
+  const xenos_status rc = cache_of(cache, "xenos_cache_write", a.c);
+  if (rc != XENOS_OK) return rc;
+  if (n_tokens < 0 || !known(dtype)) return fail(XENOS_EINVAL, "xenos_cache_write: %d tokens, type %d", n_tokens, (int)dtype);
+  if (n_tokens == 0) return XENOS_OK;
+  if (!d_k || !d_v || !d_slots) return fail(XENOS_EINVAL, "xenos_cache_write: NULL argument");
+  if (!aligned(d_k, size_of(dtype)) || !aligned(d_v, size_of(dtype)) || !aligned(d_slots, 8)) return fail(XENOS_EINVAL, "xenos_cache_write: a buffer is not aligned");
+  if (k_token_stride < 0 || k_head_stride < 0 || v_token_stride < 0 || v_head_stride < 0) return fail(XENOS_ESHAPE, "xenos_cache_write: negative stride");
+  if ((long long)n_tokens * cache->heads > 4 * kMostGroups) return fail(XENOS_EUNSUPPORTED, "xenos_cache_write: %d tokens of %d heads are more than one launch holds", n_tokens, cache->heads);
+  a.k = d_k, a.v = d_v, a.k_token = k_token_stride, a.k_head = k_head_stride, a.v_token = v_token_stride, a.v_head = v_head_stride, a.slots = d_slots, a.tokens = n_tokens;
+  return launched(launch_cache_write(a, dtype, hip_stream), "xenos_cache_write");
+}
+
+xenos_status xenos_cache_read(const xenos_cache* cache, int n_tokens, const long long* d_slots, void* d_k, void* d_v, xenos_dtype dtype, void* hip_stream) {
+  CacheReadArgs a{};
+  const xenos_status rc = cache_of(cache, "xenos_cache_read", a.c);
+  if (rc != XENOS_OK) return rc;
+  if (n_tokens < 0 || !known(dtype)) return fail(XENOS_EINVAL, "xenos_cache_read: %d tokens, type %d", n_tokens, (int)dtype);
+  if (n_tokens == 0) return XENOS_OK;
+  if (!d_k || !d_v || !d_slots) return fail(XENOS_EINVAL, "xenos_cache_read: NULL argument");
+  if (!aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_slots, 8)) return fail(XENOS_EINVAL, "xenos_cache_read: a buffer is not aligned (k and v: to 16 bytes)");
+  if ((long long)n_tokens * cache->heads > 4 * kMostGroups) return fail(XENOS_EUNSUPPORTED, "xenos_cache_read: %d tokens of %d heads are more than one launch holds", n_tokens, cache->heads);
+  a.slots = d_slots, a.k = d_k, a.v = d_v, a.tokens = n_tokens;
+  return launched(launch_cache_read(a, dtype, hip_stream), "xenos_cache_read");
 }
 
 }  // extern "C"

@@ -1,4 +1,4 @@
-"""The operators of a token model's serving step on torch tensors: 8-bit linear layers.
+"""The operators of a token model's serving step on torch tensors: 8-bit linear layers and the quantised cache of keys and values.
 
 Each function checks its tensors, allocates what it returns, and makes one or two calls of the C ABI (include/xenos.h) on torch's current
 stream of the tensors' device; nothing synchronises.  The kernels are the library's own: there is no CPU path.  Forward passes only: what
@@ -123,3 +123,55 @@ def linear(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, bias: Opt
     q, scale = quantize_rows(flat, gamma, eps)
     y = quant_matmul(q, scale, w, w_scale, cols, bias=bias, residual=residual, relu=relu, dtype=x.dtype)
     return y if x.dim() == 2 else y.view(*lead, w.shape[0])
+
+
+class KVCache:
+    """Keys and values of tokens in 8-bit integers with a scale for each token and head, in pages (the layout: xenos_cache in include/xenos.h).
+
+    The tensors are the caller's: k int8 [pages][heads][page][dim], v int8 [pages][heads][page / 16][dim][16], scales float32 [pages][heads][page].
+    Which page holds which tokens is the caller's too; a token's slot is page * page_tokens + its place in the page."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        _tensor(k, "k", None, torch.int8)
+        _need(k.dim() == 4, X.XENOS_ESHAPE, f"k is {tuple(k.shape)}, not pages x heads x tokens x dimensions")
+        n, heads, page, dim = k.shape
+        _tensor(v, "v", k, torch.int8, (n, heads, page // 16, dim, 16))
+        _tensor(k_scale, "k_scale", k, torch.float32, (n, heads, page))
+        _tensor(v_scale, "v_scale", k, torch.float32, (n, heads, page))
+        _need(page % 16 == 0 and dim % 16 == 0 and 0 < dim <= 256, X.XENOS_EUNSUPPORTED, f"pages of {page} tokens, heads of {dim} values (multiples of 16, at most 256 values)")
+        _need(k.is_contiguous() and v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous(), X.XENOS_ESHAPE, "the cache's tensors are not contiguous")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.heads, self.page_tokens, self.head_dim = n, heads, page, dim
+        self.desc = X.Cache(n, page, heads, dim, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+
+    @classmethod
+    def empty(cls, n_pages: int, page_tokens: int, heads: int, head_dim: int, device="cuda") -> "KVCache":
+        """A cache of that many pages; nothing in it is read before it is written."""
+        _need(page_tokens > 0 and page_tokens % 16 == 0, X.XENOS_EUNSUPPORTED, f"pages of {page_tokens} tokens (a multiple of 16)")
+        ints, floats = dict(dtype=torch.int8, device=device), dict(dtype=torch.float32, device=device)
+        return cls(torch.empty((n_pages, heads, page_tokens, head_dim), **ints), torch.empty((n_pages, heads, page_tokens // 16, head_dim, 16), **ints),
+                   torch.empty((n_pages, heads, page_tokens), **floats), torch.empty((n_pages, heads, page_tokens), **floats))
+
+    def write(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor):
+        """Quantises the keys and values [tokens][heads][dim] (float32 or bfloat16, any strides of tokens and heads) into the slots (int64 [tokens], each once;
+        one below 0 or beyond the cache: that token is not stored)."""
+        _float(k, "k")
+        _need(k.dim() == 3 and k.shape[1] == self.heads and k.shape[2] == self.head_dim, X.XENOS_ESHAPE, f"k is {tuple(k.shape)}, not tokens x {self.heads} x {self.head_dim}")
+        _tensor(k, "k", self.k)
+        _tensor(v, "v", self.k, k.dtype, k.shape)
+        _tensor(slots, "slots", self.k, torch.int64, k.shape[:1])
+        k, v, slots = k if k.stride(2) == 1 else k.contiguous(), v if v.stride(2) == 1 else v.contiguous(), slots.contiguous()
+        with _on(k):
+            X.xenos_cache_write(self.desc, k.shape[0], k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), _DTYPE[k.dtype],
+                                slots.data_ptr(), _stream(k))
+
+    def read(self, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16) -> Tuple[torch.Tensor, torch.Tensor]:
+        """The keys and values of the slots (int64 [tokens]) as the numbers they stand for, [tokens][heads][dim] each; zeros for a slot that is none."""
+        _tensor(slots, "slots", self.k, torch.int64)
+        _need(slots.dim() == 1, X.XENOS_ESHAPE, f"slots is {tuple(slots.shape)}, not a list")
+        _need(dtype in _DTYPE, X.XENOS_EUNSUPPORTED, f"{dtype}: float32 and bfloat16 are supported")
+        slots = slots.contiguous()
+        k, v = (torch.empty((slots.shape[0], self.heads, self.head_dim), dtype=dtype, device=slots.device) for _ in range(2))
+        with _on(slots):
+            X.xenos_cache_read(self.desc, slots.shape[0], slots.data_ptr(), k.data_ptr(), v.data_ptr(), _DTYPE[dtype], _stream(slots))
+        return k, v

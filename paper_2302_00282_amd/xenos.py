@@ -60,6 +60,11 @@ class QuantMatmulArgs(C.Structure):
                 ("relu", C.c_int), ("dtype", C.c_int), ("d_out", C.c_void_p), ("out_stride", C.c_longlong)]
 
 
+class Cache(C.Structure):
+    _fields_ = [("n_pages", C.c_int), ("page_tokens", C.c_int), ("heads", C.c_int), ("head_dim", C.c_int),
+                ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p)]
+
+
 class XenosError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"xenos status {status}: {msg}")
@@ -97,12 +102,15 @@ def lib():
         L.xenos_probe_read.argtypes = [C.POINTER(HwInfo), vp, C.c_size_t, vp, C.c_size_t, vp]
         L.xenos_quant_rows.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_longlong, vp, C.c_float, vp, vp, vp]
         L.xenos_quant_matmul.argtypes = [C.POINTER(QuantMatmulArgs), vp]
+        L.xenos_cache_write.argtypes = [C.POINTER(Cache), C.c_int, vp, C.c_longlong, C.c_longlong, vp, C.c_longlong, C.c_longlong, C.c_int, vp, vp]
+        L.xenos_cache_read.argtypes = [C.POINTER(Cache), C.c_int, vp, vp, vp, C.c_int, vp]
         L.xenos_destroy.argtypes = [vp]
         L.xenos_destroy.restype = None
         L.xenos_last_error.restype = C.c_char_p
         for f in ("xenos_graph_create", "xenos_plan_link_split", "xenos_plan_query", "xenos_plan_bind",
                   "xenos_run", "xenos_run_graph", "xenos_run_static", "xenos_run_with", "xenos_run_chain", "xenos_plan_tune",
-                  "xenos_probe_mfma", "xenos_probe_read", "xenos_quant_rows", "xenos_quant_matmul"):
+                  "xenos_probe_mfma", "xenos_probe_read", "xenos_quant_rows", "xenos_quant_matmul",
+                  "xenos_cache_write", "xenos_cache_read"):
             getattr(L, f).restype = C.c_int
         _lib = L
     return _lib
@@ -204,6 +212,15 @@ def xenos_quant_rows(d_x: int, dtype: int, rows: int, cols: int, row_stride: int
 
 def xenos_quant_matmul(args: QuantMatmulArgs, stream: int = 0):
     _check(lib().xenos_quant_matmul(C.byref(args), stream))
+
+
+def xenos_cache_write(cache: Cache, n_tokens: int, d_k: int, k_token_stride: int, k_head_stride: int, d_v: int, v_token_stride: int, v_head_stride: int,
+                      dtype: int, d_slots: int, stream: int = 0):
+    _check(lib().xenos_cache_write(C.byref(cache), n_tokens, d_k, k_token_stride, k_head_stride, d_v, v_token_stride, v_head_stride, dtype, d_slots, stream))
+
+
+def xenos_cache_read(cache: Cache, n_tokens: int, d_slots: int, d_k: int, d_v: int, dtype: int, stream: int = 0):
+    _check(lib().xenos_cache_read(C.byref(cache), n_tokens, d_slots, d_k, d_v, dtype, stream))
 
 
 def xenos_destroy(handle: Optional[int]):
