@@ -279,6 +279,18 @@ xenos_status xenos_cache_write(const xenos_cache* cache, int n_tokens, const voi
 /* The rows of n_tokens slots as the values they stand for, [n_tokens][heads][head_dim] of k and of v; a slot below 0 or beyond the cache reads zeros. */
 xenos_status xenos_cache_read(const xenos_cache* cache, int n_tokens, const long long* d_slots, void* d_k, void* d_v, xenos_dtype dtype, void* hip_stream);
 
+/* What is read from the logits of `rows` positions over `vocab` tokens (row_stride elements apart):
+ *   d_logprob[r]   log softmax(x[r])[d_targets[r]]; 0 where the target lies outside 0 .. vocab - 1 (no token given)
+ *   d_entropy[r]   - sum p log p; what has p = 0 (logits of -infinity: forbidden tokens) adds nothing
+ *   d_top_token[r][i], d_top_logprob[r][i]   the `top` most likely tokens (0 .. XENOS_TOP_MAX, at most vocab), best first, equal ones by the lowest index
+ * d_targets with d_logprob, and d_entropy, may be NULL: not wanted.  A row with a NaN, with an infinity or with nothing but -infinity has no distribution: its
+ * logarithms and entropy are NaN (its tokens are still in order, NaN before everything).  One pass over the logits; sums in fp32.
+ * Few rows are shared out over the units in parts: d_workspace (4-byte aligned) then has to hold *bytes of xenos_logprobs_workspace, which may be 0. */
+#define XENOS_TOP_MAX 64
+xenos_status xenos_logprobs_workspace(int rows, int vocab, int top, size_t* bytes);
+xenos_status xenos_logprobs(const void* d_logits, xenos_dtype dtype, int rows, int vocab, long long row_stride, const long long* d_targets, int top,
+                            float* d_logprob, float* d_entropy, float* d_top_logprob, int* d_top_token, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Releases a graph or a plan (either handle type; NULL is ignored).  A plan holds a reference to
  * nothing of the graph after xenos_plan_link_split returns. */
 void xenos_destroy(void* graph_or_plan);

@@ -51,6 +51,22 @@ struct CacheReadArgs {
   void *k, *v;                                               // [tokens][heads][dim], 16-byte aligned
   int tokens;
 };
+struct LogprobsArgs {
+  const void* x;                                             // [rows][stride], `vocab` of each row
+  const long long* targets;                                  // [rows] or null
+  float *logprob, *entropy;                                  // [rows] or null
+  float* top_logprob;                                        // [rows][top]
+  int* top_token;
+  uint32_t* part;                                            // [rows][parts][logprobs_part_words(top)], unless parts = 1
+  long long stride;
+  int rows, vocab, top;
+  int parts, part_len;                                       // a row is read in `parts` pieces of part_len
+};
+constexpr int kTopMost = 64;
+inline int logprobs_part_words(int top) { return 3 + 2 * top; }
+void logprobs_split(int rows, int vocab, int* parts, int* part_len);
+int launch_logprobs(const LogprobsArgs& a, int dtype, void* stream);
+
 int launch_cache_write(const CacheWriteArgs& a, int dtype, void* stream);
 int launch_cache_read(const CacheReadArgs& a, int dtype, void* stream);
 

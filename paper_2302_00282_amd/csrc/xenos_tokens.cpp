@@ -96,4 +96,31 @@ xenos_status xenos_cache_read(const xenos_cache* cache, int n_tokens, const long
   return launched(launch_cache_read(a, dtype, hip_stream), "xenos_cache_read");
 }
 
+xenos_status xenos_logprobs_workspace(int rows, int vocab, int top, size_t* bytes) {
+  if (rows < 0 || vocab <= 0 || top < 0 || top > XENOS_TOP_MAX || top > vocab || !bytes)
+    return fail(XENOS_EINVAL, "xenos_logprobs_workspace: %d rows of %d tokens, the best %d", rows, vocab, top);
+  int parts, len;
+  logprobs_split(rows, vocab, &parts, &len);
+  *bytes = parts > 1 ? (size_t)rows * parts * logprobs_part_words(top) * 4 : 0;
+  return XENOS_OK;
+}
+
+xenos_status xenos_logprobs(const void* d_logits, xenos_dtype dtype, int rows, int vocab, long long row_stride, const long long* d_targets, int top,
+                            float* d_logprob, float* d_entropy, float* d_top_logprob, int* d_top_token, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  if (rows < 0 || vocab <= 0 || top < 0 || top > XENOS_TOP_MAX || !known(dtype)) return fail(XENOS_EINVAL, "xenos_logprobs: %d rows of %d tokens, the best %d, type %d", rows, vocab, top, (int)dtype);
+  if (top > vocab) return fail(XENOS_ESHAPE, "xenos_logprobs: the best %d of %d tokens", top, vocab);
+  if (vocab > (1 << 30)) return fail(XENOS_EUNSUPPORTED, "xenos_logprobs: %d tokens", vocab);
+  if (rows == 0) return XENOS_OK;
+  if (!d_logits || !d_targets != !d_logprob || (top && (!d_top_logprob || !d_top_token))) return fail(XENOS_EINVAL, "xenos_logprobs: NULL argument");
+  if (rows > 1 && row_stride < vocab) return fail(XENOS_ESHAPE, "xenos_logprobs: rows of %d elements, %lld apart", vocab, row_stride);
+  if (!aligned(d_logits, size_of(dtype)) || !aligned(d_targets, 8) || !aligned(d_logprob, 4) || !aligned(d_entropy, 4) || !aligned(d_top_logprob, 4) || !aligned(d_top_token, 4) || !aligned(d_workspace, 4))
+    return fail(XENOS_EINVAL, "xenos_logprobs: a buffer is not aligned");
+  LogprobsArgs a{d_logits, d_targets, d_logprob, d_entropy, d_top_logprob, d_top_token, (uint32_t*)d_workspace, rows > 1 ? row_stride : 0, rows, vocab, top, 1, vocab};
+  logprobs_split(rows, vocab, &a.parts, &a.part_len);
+  if ((long long)rows * a.parts > kMostGroups) return fail(XENOS_EUNSUPPORTED, "xenos_logprobs: %d rows are more than one launch holds", rows);
+  const size_t need = a.parts > 1 ? (size_t)rows * a.parts * logprobs_part_words(top) * 4 : 0;
+  if (need && (!d_workspace || workspace_bytes < need)) return fail(XENOS_EINVAL, "xenos_logprobs: a workspace of %zu bytes, %zu are needed", workspace_bytes, need);
+  return launched(launch_logprobs(a, dtype, hip_stream), "xenos_logprobs");
+}
+
 }  // extern "C"

@@ -1,4 +1,5 @@
-"""The operators of a token model's serving step on torch tensors: 8-bit linear layers and the quantised cache of keys and values.
+"""The operators of a token model's serving step on torch tensors: 8-bit linear layers, the quantised cache of keys and values, and what
+is read from the logits.
 
 Each function checks its tensors, allocates what it returns, and makes one or two calls of the C ABI (include/xenos.h) on torch's current
 stream of the tensors' device; nothing synchronises.  The kernels are the library's own: there is no CPU path.  Forward passes only: what
@@ -175,3 +176,31 @@ class KVCache:
         with _on(slots):
             X.xenos_cache_read(self.desc, slots.shape[0], slots.data_ptr(), k.data_ptr(), v.data_ptr(), _DTYPE[dtype], _stream(slots))
         return k, v
+
+
+def logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0):
+    """Log probabilities of given tokens, entropy, and the likeliest tokens of each position: logits [positions][vocab] (float32 or bfloat16, any row stride),
+    targets int64 [positions] or None.
+
+    Returns (logprob float32 [positions] or None, entropy float32 [positions], top_logprob float32 [positions][top], top_token int32 [positions][top]): the tokens
+    from the likeliest on, equal ones by the lowest index.  A target outside 0 .. vocab - 1 is none, and its logprob 0."""
+    _float(logits, "logits")
+    _need(logits.dim() == 2 and logits.shape[1] > 0, X.XENOS_ESHAPE, f"logits is {tuple(logits.shape)}, not positions x tokens")
+    rows, vocab = logits.shape
+    _need(0 <= top <= X.XENOS_TOP_MAX, X.XENOS_EUNSUPPORTED, f"the best {top} tokens (at most {X.XENOS_TOP_MAX})")
+    _need(top <= vocab, X.XENOS_ESHAPE, f"the best {top} of {vocab} tokens")
+    if targets is not None:
+        _tensor(targets, "targets", logits, torch.int64, (rows,))
+        targets = targets.contiguous()
+    if logits.stride(1) != 1 or (rows > 1 and logits.stride(0) < vocab):
+        logits = logits.contiguous()
+    floats = dict(dtype=torch.float32, device=logits.device)
+    given = None if targets is None else torch.empty(rows, **floats)
+    entropy, best = torch.empty(rows, **floats), torch.empty((rows, top), **floats)
+    token = torch.empty((rows, top), dtype=torch.int32, device=logits.device)
+    need = X.xenos_logprobs_workspace(rows, vocab, top)
+    workspace = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
+    with _on(logits):
+        X.xenos_logprobs(logits.data_ptr(), _DTYPE[logits.dtype], rows, vocab, logits.stride(0), _ptr(targets), top, _ptr(given), entropy.data_ptr(),
+                         best.data_ptr(), token.data_ptr(), _ptr(workspace), need, _stream(logits))
+    return given, entropy, best, token

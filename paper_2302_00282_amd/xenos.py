@@ -104,13 +104,15 @@ def lib():
         L.xenos_quant_matmul.argtypes = [C.POINTER(QuantMatmulArgs), vp]
         L.xenos_cache_write.argtypes = [C.POINTER(Cache), C.c_int, vp, C.c_longlong, C.c_longlong, vp, C.c_longlong, C.c_longlong, C.c_int, vp, vp]
         L.xenos_cache_read.argtypes = [C.POINTER(Cache), C.c_int, vp, vp, vp, C.c_int, vp]
+        L.xenos_logprobs_workspace.argtypes = [C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
+        L.xenos_logprobs.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_longlong, vp, C.c_int, vp, vp, vp, vp, vp, C.c_size_t, vp]
         L.xenos_destroy.argtypes = [vp]
         L.xenos_destroy.restype = None
         L.xenos_last_error.restype = C.c_char_p
         for f in ("xenos_graph_create", "xenos_plan_link_split", "xenos_plan_query", "xenos_plan_bind",
                   "xenos_run", "xenos_run_graph", "xenos_run_static", "xenos_run_with", "xenos_run_chain", "xenos_plan_tune",
                   "xenos_probe_mfma", "xenos_probe_read", "xenos_quant_rows", "xenos_quant_matmul",
-                  "xenos_cache_write", "xenos_cache_read"):
+                  "xenos_cache_write", "xenos_cache_read", "xenos_logprobs_workspace", "xenos_logprobs"):
             getattr(L, f).restype = C.c_int
         _lib = L
     return _lib
@@ -221,6 +223,21 @@ def xenos_cache_write(cache: Cache, n_tokens: int, d_k: int, k_token_stride: int
 
 def xenos_cache_read(cache: Cache, n_tokens: int, d_slots: int, d_k: int, d_v: int, dtype: int, stream: int = 0):
     _check(lib().xenos_cache_read(C.byref(cache), n_tokens, d_slots, d_k, d_v, dtype, stream))
+
+
+XENOS_TOP_MAX = 64
+
+
+def xenos_logprobs_workspace(rows: int, vocab: int, top: int) -> int:
+    n = C.c_size_t()
+    _check(lib().xenos_logprobs_workspace(rows, vocab, top, C.byref(n)))
+    return n.value
+
+
+def xenos_logprobs(d_logits: int, dtype: int, rows: int, vocab: int, row_stride: int, d_targets: int, top: int, d_logprob: int, d_entropy: int,
+                   d_top_logprob: int, d_top_token: int, d_workspace: int = 0, workspace_bytes: int = 0, stream: int = 0):
+    _check(lib().xenos_logprobs(d_logits, dtype, rows, vocab, row_stride, d_targets, top, d_logprob, d_entropy, d_top_logprob, d_top_token,
+                                d_workspace, workspace_bytes, stream))
 
 
 def xenos_destroy(handle: Optional[int]):
