@@ -263,7 +263,7 @@ xenos_status xenos_quant_matmul(const xenos_quant_matmul_args* args, void* hip_s
  *   k       int8 [n_pages][heads][page_tokens][head_dim]
  *   v       int8 [n_pages][heads][page_tokens / 16][head_dim][16]     (16 tokens of one dimension side by side)
  *   scales  fp32 [n_pages][heads][page_tokens] each
- * page_tokens: a multiple of 16; head_dim: a multiple of 16 up to 256; k and v 16-byte aligned.  Nothing has to be cleared: what no length
+ * page_tokens: a multiple of 16; head_dim: a multiple of 16 up to 256; all four 16-byte aligned.  Nothing has to be cleared: what no length
  * names is not looked at, whatever bits it holds. */
 typedef struct {
   int n_pages, page_tokens, heads, head_dim;
@@ -278,6 +278,36 @@ xenos_status xenos_cache_write(const xenos_cache* cache, int n_tokens, const voi
 
 /* The rows of n_tokens slots as the values they stand for, [n_tokens][heads][head_dim] of k and of v; a slot below 0 or beyond the cache reads zeros. */
 xenos_status xenos_cache_read(const xenos_cache* cache, int n_tokens, const long long* d_slots, void* d_k, void* d_v, xenos_dtype dtype, void* hip_stream);
+
+/* Attention of query rows to the keys of a cache, for a batch of sequences that may begin with the same tokens:
+ *   out[t][h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * q[t][h] . k_j - max),   over the keys that t sees, in head h / (heads / cache heads) of the cache.
+ * Sequence b has lengths[b] tokens of its own behind the shared prefix, page table[b * table_stride + i] holding tokens i * page_tokens and on; its
+ * queries, rows starts[b] .. starts[b + 1] - 1 of q (starts NULL: row b), are the last of those tokens: query i of m sees the whole
+ * prefix and the sequence's tokens up to lengths[b] - m + i.  The prefix (prefix_length tokens in the pages of d_prefix_table; 0: none) is read once for all sequences.
+ * A query that sees nothing gets zeros.  Tokens beyond the table, and those of a page that is none of the cache's, are not seen.
+ * q and out: element (t, h, d) at t * token_stride + h * head_stride + d, bf16 (the only type: the keys are 8 bits); out must not overlap q.
+ * Sums, maxima and the normaliser are fp32; probabilities are rounded to fp16 (relative to the largest value scale) for the product with the values.
+ * max_queries and max_length: no sequence has more queries, or tokens of its own.  They choose how the work is shared out, before the lengths are known to the host;
+ * lengths and starts stay on the device, so that a captured graph can be replayed as sequences grow.
+ * d_workspace: 16-byte aligned, *bytes of xenos_attention_workspace (which reads no device memory); may be 0. */
+typedef struct {
+  int n_seqs, n_queries, heads;            /* n_queries: rows of q                   */
+  xenos_dtype dtype;
+  const void* d_q;
+  long long q_token_stride, q_head_stride;
+  void* d_out;
+  long long out_token_stride, out_head_stride;
+  const int* d_starts;                     /* [n_seqs + 1], ascending, or NULL       */
+  const int* d_lengths;                    /* [n_seqs]                               */
+  const int* d_tables;                     /* [n_seqs][table_stride]                 */
+  int table_stride;                        /* pages                                  */
+  int max_queries, max_length;
+  const int* d_prefix_table;
+  int prefix_length;
+  float scale;
+} xenos_attention_args;
+xenos_status xenos_attention_workspace(const xenos_cache* cache, const xenos_attention_args* args, size_t* bytes);
+xenos_status xenos_attention(const xenos_cache* cache, const xenos_attention_args* args, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
 /* What is read from the logits of `rows` positions over `vocab` tokens (row_stride elements apart):
  *   d_logprob[r]   log softmax(x[r])[d_targets[r]]; 0 where the target lies outside 0 .. vocab - 1 (no token given)

@@ -34,7 +34,7 @@ struct QuantMatmulArgs {
 int launch_quant_matmul(const QuantMatmulArgs& a, int dtype, void* stream);
 
 struct CacheArgs {
-  int8_t *k, *v;                                             // 16-byte aligned, the layouts of xenos.h
+  int8_t *k, *v;                                             // 16-byte aligned, as the scales are; the layouts of xenos.h
   float *k_scale, *v_scale;
   int n_pages, page, heads, dim;                             // page and dim are multiples of 16, dim <= 256
 };
@@ -51,6 +51,29 @@ struct CacheReadArgs {
   void *k, *v;                                               // [tokens][heads][dim], 16-byte aligned
   int tokens;
 };
+// A segment of keys that the row tiles of an attention call pass over: the shared prefix, or the sequences' own tokens.
+struct AttentionShare {
+  int tiles;                                                 // of rows
+  int parts, part_len;                                       // pieces of the keys, of part_len (a multiple of 64) tokens each, the last one to the end
+  int whole;                                                 // the wavefronts of a workgroup have the same rows and take turns with the keys; else each has rows of its own
+};
+struct AttentionArgs {
+  CacheArgs c;
+  const uint16_t* q;
+  uint16_t* out;
+  long long q_token, q_head, out_token, out_head;
+  const int *starts, *lengths, *tables, *prefix_table;
+  float* part;                                               // [row][slot](dim + 2 floats): unless there is one slot
+  int n_seqs, n_queries, heads, group, table_stride, prefix_len;
+  int vec_q, vec_out;                                        // rows of q are 16-byte, of out 8-byte aligned
+  float scale2;                                              // scale log2 e
+  int row_tiles;                                             // of 16 rows, per wavefront: 1 or 2
+  AttentionShare own, prefix;
+};
+inline int attention_slots(const AttentionArgs& a) { return a.own.parts + a.prefix.parts; }
+void attention_split(AttentionArgs& a, int max_queries, int max_length);
+int launch_attention(const AttentionArgs& a, void* stream);
+
 struct LogprobsArgs {
   const void* x;                                             // [rows][stride], `vocab` of each row
   const long long* targets;                                  // [rows] or null

@@ -25,9 +25,31 @@ xenos_status cache_of(const xenos_cache* c, const char* who, CacheArgs& a) {
   if (c->page_tokens % 16 || c->head_dim % 16 || c->head_dim > 256)
     return fail(XENOS_EUNSUPPORTED, "%s: pages of %d tokens, heads of %d values (multiples of 16, at most 256 values)", who, c->page_tokens, c->head_dim);
   if (c->n_pages > 0 && (!c->d_k || !c->d_v || !c->d_k_scale || !c->d_v_scale)) return fail(XENOS_EINVAL, "%s: NULL cache buffer", who);
-  if (!aligned(c->d_k, 16) || !aligned(c->d_v, 16) || !aligned(c->d_k_scale, 4) || !aligned(c->d_v_scale, 4))
-    return fail(XENOS_EINVAL, "%s: a cache buffer is not aligned (k and v: to 16 bytes)", who);
+  if (!aligned(c->d_k, 16) || !aligned(c->d_v, 16) || !aligned(c->d_k_scale, 16) || !aligned(c->d_v_scale, 16))
+    return fail(XENOS_EINVAL, "%s: a cache buffer is not aligned to 16 bytes", who);
   a = CacheArgs{(int8_t*)c->d_k, (int8_t*)c->d_v, c->d_k_scale, c->d_v_scale, c->n_pages, c->page_tokens, c->heads, c->head_dim};
+  return XENOS_OK;
+}
+
+// Everything of the arguments that can be told without the device's memory.
+xenos_status attention_of(const xenos_cache* cache, const xenos_attention_args* p, const char* who, AttentionArgs& a, size_t* bytes) {
+  const xenos_status rc = cache_of(cache, who, a.c);
+  if (rc != XENOS_OK) return rc;
+  if (!p || p->n_seqs < 0 || p->n_queries < 0 || p->heads <= 0 || !known(p->dtype) || p->table_stride < 0 || p->max_queries < 0 || p->max_length < 0 || p->prefix_length < 0)
+    return fail(XENOS_EINVAL, "%s: bad argument", who);
+  if (p->dtype != XENOS_BF16) return fail(XENOS_EUNSUPPORTED, "%s: queries are bf16", who);
+  if (p->heads % cache->heads) return fail(XENOS_ESHAPE, "%s: %d heads over %d heads of the cache", who, p->heads, cache->heads);
+  if (p->max_length > (1 << 30) || p->prefix_length > (1 << 30) || (long long)p->n_queries * p->heads > (1 << 28))
+    return fail(XENOS_EUNSUPPORTED, "%s: %d queries of %d heads, %d and %d tokens", who, p->n_queries, p->heads, p->max_length, p->prefix_length);
+  if (p->n_queries > 0 && p->n_seqs == 0) return fail(XENOS_ESHAPE, "%s: %d queries of no sequence", who, p->n_queries);
+  if (!p->d_starts && p->n_queries != p->n_seqs) return fail(XENOS_ESHAPE, "%s: %d queries of %d sequences, and no starts", who, p->n_queries, p->n_seqs);
+  a.n_seqs = p->n_seqs, a.n_queries = p->n_queries, a.heads = p->heads, a.group = p->heads / cache->heads, a.table_stride = p->table_stride;
+  a.prefix_len = p->prefix_length;
+  attention_split(a, std::min(p->max_queries, p->n_queries), (int)std::min<long long>(p->max_length, (long long)p->table_stride * cache->page_tokens));
+  const long long own = (long long)a.n_seqs * a.own.tiles * a.own.parts, front = (long long)a.prefix.tiles * a.prefix.parts;
+  if ((own + front) * cache->heads > kMostGroups || (long long)p->n_queries * p->heads > 4 * kMostGroups)
+    return fail(XENOS_EUNSUPPORTED, "%s: %d queries of %d sequences are more than one launch holds", who, p->n_queries, p->n_seqs);
+  *bytes = attention_slots(a) > 1 ? (size_t)p->n_queries * p->heads * attention_slots(a) * (cache->head_dim + 2) * 4 : 0;
   return XENOS_OK;
 }
 
@@ -94,6 +116,39 @@ xenos_status xenos_cache_read(const xenos_cache* cache, int n_tokens, const long
   if ((long long)n_tokens * cache->heads > 4 * kMostGroups) return fail(XENOS_EUNSUPPORTED, "xenos_cache_read: %d tokens of %d heads are more than one launch holds", n_tokens, cache->heads);
   a.slots = d_slots, a.k = d_k, a.v = d_v, a.tokens = n_tokens;
   return launched(launch_cache_read(a, dtype, hip_stream), "xenos_cache_read");
+}
+
+xenos_status xenos_attention_workspace(const xenos_cache* cache, const xenos_attention_args* args, size_t* bytes) {
+  AttentionArgs a{};
+  size_t need;
+  if (!bytes) return fail(XENOS_EINVAL, "xenos_attention_workspace: NULL argument");
+  const xenos_status rc = attention_of(cache, args, "xenos_attention_workspace", a, &need);
+  if (rc == XENOS_OK) *bytes = need;
+  return rc;
+}
+
+xenos_status xenos_attention(const xenos_cache* cache, const xenos_attention_args* p, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  AttentionArgs a{};
+  size_t need = 0;
+  const xenos_status rc = attention_of(cache, p, "xenos_attention", a, &need);
+  if (rc != XENOS_OK) return rc;
+  if (p->n_queries == 0 || p->n_seqs == 0) return XENOS_OK;
+  if (!p->d_q || !p->d_out || !p->d_lengths || (p->table_stride > 0 && !p->d_tables) || (p->prefix_length > 0 && !p->d_prefix_table))
+    return fail(XENOS_EINVAL, "xenos_attention: NULL argument");
+  if (!aligned(p->d_q, 2) || !aligned(p->d_out, 2) || !aligned(p->d_starts, 4) || !aligned(p->d_lengths, 4) || !aligned(p->d_tables, 4) || !aligned(p->d_prefix_table, 4) ||
+      !aligned(d_workspace, 16))
+    return fail(XENOS_EINVAL, "xenos_attention: a buffer is not aligned (the workspace: to 16 bytes)");
+  if (p->q_token_stride < 0 || p->q_head_stride < 0 || p->out_token_stride < 0 || p->out_head_stride < 0) return fail(XENOS_ESHAPE, "xenos_attention: negative stride");
+  if ((p->heads > 1 && p->out_head_stride < cache->head_dim) || (p->n_queries > 1 && p->out_token_stride < cache->head_dim))
+    return fail(XENOS_ESHAPE, "xenos_attention: rows of out overlap (%d values, %lld and %lld apart)", cache->head_dim, p->out_token_stride, p->out_head_stride);
+  if (need && (!d_workspace || workspace_bytes < need)) return fail(XENOS_EINVAL, "xenos_attention: a workspace of %zu bytes, %zu are needed", workspace_bytes, need);
+  a.q = (const uint16_t*)p->d_q, a.out = (uint16_t*)p->d_out;
+  a.q_token = p->q_token_stride, a.q_head = p->q_head_stride, a.out_token = p->out_token_stride, a.out_head = p->out_head_stride;
+  a.starts = p->d_starts, a.lengths = p->d_lengths, a.tables = p->d_tables, a.prefix_table = p->d_prefix_table, a.part = (float*)d_workspace;
+  a.vec_q = aligned(a.q, 16) && a.q_token % 8 == 0 && a.q_head % 8 == 0;
+  a.vec_out = aligned(a.out, 8) && a.out_token % 4 == 0 && a.out_head % 4 == 0;
+  a.scale2 = p->scale * 1.44269504088896340736f;
+  return launched(launch_attention(a, hip_stream), "xenos_attention");
 }
 
 xenos_status xenos_logprobs_workspace(int rows, int vocab, int top, size_t* bytes) {

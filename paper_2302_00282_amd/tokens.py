@@ -1,5 +1,5 @@
-"""The operators of a token model's serving step on torch tensors: 8-bit linear layers, the quantised cache of keys and values, and what
-is read from the logits.
+"""The operators of a token model's serving step on torch tensors: 8-bit linear layers, the quantised cache of keys and values, the
+attention that reads it, and what is read from the logits.
 
 Each function checks its tensors, allocates what it returns, and makes one or two calls of the C ABI (include/xenos.h) on torch's current
 stream of the tensors' device; nothing synchronises.  The kernels are the library's own: there is no CPU path.  Forward passes only: what
@@ -7,6 +7,7 @@ they return carries no gradient, and an input that asks for one is refused.
 """
 from __future__ import annotations
 
+import math
 from contextlib import nullcontext
 from typing import Optional, Tuple
 
@@ -176,6 +177,47 @@ class KVCache:
         with _on(slots):
             X.xenos_cache_read(self.desc, slots.shape[0], slots.data_ptr(), k.data_ptr(), v.data_ptr(), _DTYPE[dtype], _stream(slots))
         return k, v
+
+
+def attention(q: torch.Tensor, cache: KVCache, tables: torch.Tensor, lengths: torch.Tensor, *, starts: Optional[torch.Tensor] = None, max_queries: int = 1,
+              max_length: Optional[int] = None, prefix_table: Optional[torch.Tensor] = None, prefix_length: int = 0, scale: Optional[float] = None,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of q bfloat16 [queries][heads][dim] (any strides of tokens and heads) to the cache; heads: a multiple of the cache's. Returns [queries][heads][dim].
+
+    Sequence b has lengths[b] (int32 [sequences]) tokens in the pages tables[b] (int32 [sequences][pages], entries behind its last page are not looked at) behind `prefix_length`
+    tokens in the pages `prefix_table` (int32) that all sequences share.  Its queries, rows starts[b] .. starts[b + 1] of q (int32 [sequences + 1]; None: row b alone), are the last of
+    its tokens, already in the cache, and each sees the prefix and the tokens up to itself.  max_queries, max_length: what no sequence exceeds
+    (max_length None: what its table holds); they decide how the work is shared out and cost no look at the lengths.  scale: None is 1 / sqrt(dim)."""
+    _tensor(q, "q", cache.k)
+    _need(q.dtype == torch.bfloat16, X.XENOS_EUNSUPPORTED, f"q is {q.dtype}: bfloat16 is supported")
+    _need(q.dim() == 3 and q.shape[2] == cache.head_dim and q.shape[1] > 0 and q.shape[1] % cache.heads == 0, X.XENOS_ESHAPE,
+          f"q is {tuple(q.shape)}, not queries x a multiple of {cache.heads} heads x {cache.head_dim}")
+    _tensor(lengths, "lengths", q, torch.int32)
+    _tensor(tables, "tables", q, torch.int32)
+    _need(lengths.dim() == 1 and tables.dim() == 2 and tables.shape[0] == lengths.shape[0], X.XENOS_ESHAPE, f"{tuple(tables.shape)} tables of {tuple(lengths.shape)} sequences")
+    n_seqs, n_queries = lengths.shape[0], q.shape[0]
+    starts = _packed(starts, "starts", q, (n_seqs + 1,), torch.int32)
+    _need(starts is not None or n_queries == n_seqs, X.XENOS_ESHAPE, f"{n_queries} queries of {n_seqs} sequences, and no starts")
+    if prefix_table is not None:
+        _tensor(prefix_table, "prefix_table", q, torch.int32)
+        prefix_table = prefix_table.contiguous()
+    held = 0 if prefix_table is None else prefix_table.numel() * cache.page_tokens
+    _need(0 <= prefix_length <= held, X.XENOS_ESHAPE, f"a prefix of {prefix_length} tokens in pages of {held}")
+    q = q if q.stride(2) == 1 else q.contiguous()
+    tables, lengths = tables.contiguous(), lengths.contiguous()
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    else:
+        _tensor(out, "out", q, q.dtype, q.shape)
+        _need(out.stride(2) == 1, X.XENOS_ESHAPE, "the rows of out are not contiguous")
+    args = X.AttentionArgs(n_seqs, n_queries, q.shape[1], X.XENOS_BF16, q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1),
+                           _ptr(starts), lengths.data_ptr(), tables.data_ptr(), tables.shape[1], max_queries, tables.shape[1] * cache.page_tokens if max_length is None else max_length,
+                           _ptr(prefix_table), prefix_length, 1.0 / math.sqrt(cache.head_dim) if scale is None else scale)
+    need = X.xenos_attention_workspace(cache.desc, args)
+    workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    with _on(q):
+        X.xenos_attention(cache.desc, args, _ptr(workspace), need, _stream(q))
+    return out
 
 
 def logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0):

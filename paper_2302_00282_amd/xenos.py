@@ -65,6 +65,14 @@ class Cache(C.Structure):
                 ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p)]
 
 
+class AttentionArgs(C.Structure):
+    _fields_ = [("n_seqs", C.c_int), ("n_queries", C.c_int), ("heads", C.c_int), ("dtype", C.c_int),
+                ("d_q", C.c_void_p), ("q_token_stride", C.c_longlong), ("q_head_stride", C.c_longlong),
+                ("d_out", C.c_void_p), ("out_token_stride", C.c_longlong), ("out_head_stride", C.c_longlong),
+                ("d_starts", C.c_void_p), ("d_lengths", C.c_void_p), ("d_tables", C.c_void_p), ("table_stride", C.c_int),
+                ("max_queries", C.c_int), ("max_length", C.c_int), ("d_prefix_table", C.c_void_p), ("prefix_length", C.c_int), ("scale", C.c_float)]
+
+
 class XenosError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"xenos status {status}: {msg}")
@@ -106,13 +114,16 @@ def lib():
         L.xenos_cache_read.argtypes = [C.POINTER(Cache), C.c_int, vp, vp, vp, C.c_int, vp]
         L.xenos_logprobs_workspace.argtypes = [C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
         L.xenos_logprobs.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_longlong, vp, C.c_int, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.xenos_attention_workspace.argtypes = [C.POINTER(Cache), C.POINTER(AttentionArgs), C.POINTER(C.c_size_t)]
+        L.xenos_attention.argtypes = [C.POINTER(Cache), C.POINTER(AttentionArgs), vp, C.c_size_t, vp]
         L.xenos_destroy.argtypes = [vp]
         L.xenos_destroy.restype = None
         L.xenos_last_error.restype = C.c_char_p
         for f in ("xenos_graph_create", "xenos_plan_link_split", "xenos_plan_query", "xenos_plan_bind",
                   "xenos_run", "xenos_run_graph", "xenos_run_static", "xenos_run_with", "xenos_run_chain", "xenos_plan_tune",
                   "xenos_probe_mfma", "xenos_probe_read", "xenos_quant_rows", "xenos_quant_matmul",
-                  "xenos_cache_write", "xenos_cache_read", "xenos_logprobs_workspace", "xenos_logprobs"):
+                  "xenos_cache_write", "xenos_cache_read", "xenos_logprobs_workspace", "xenos_logprobs",
+                  "xenos_attention_workspace", "xenos_attention"):
             getattr(L, f).restype = C.c_int
         _lib = L
     return _lib
@@ -223,6 +234,16 @@ def xenos_cache_write(cache: Cache, n_tokens: int, d_k: int, k_token_stride: int
 
 def xenos_cache_read(cache: Cache, n_tokens: int, d_slots: int, d_k: int, d_v: int, dtype: int, stream: int = 0):
     _check(lib().xenos_cache_read(C.byref(cache), n_tokens, d_slots, d_k, d_v, dtype, stream))
+
+
+def xenos_attention_workspace(cache: Cache, args: AttentionArgs) -> int:
+    n = C.c_size_t()
+    _check(lib().xenos_attention_workspace(C.byref(cache), C.byref(args), C.byref(n)))
+    return n.value
+
+
+def xenos_attention(cache: Cache, args: AttentionArgs, d_workspace: int = 0, workspace_bytes: int = 0, stream: int = 0):
+    _check(lib().xenos_attention(C.byref(cache), C.byref(args), d_workspace, workspace_bytes, stream))
 
 
 XENOS_TOP_MAX = 64
