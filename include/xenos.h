@@ -257,6 +257,27 @@ typedef struct {
 } xenos_quant_matmul_args;
 xenos_status xenos_quant_matmul(const xenos_quant_matmul_args* args, void* hip_stream);
 
+/* A linear layer: xenos_quant_rows of the tokens x and xenos_quant_matmul with the weights, in one call (few short rows: in one launch).  The members mean
+ * what they mean there; out must not overlap x.  d_workspace: 16-byte aligned, *bytes of xenos_linear_workspace, which may be 0. */
+typedef struct {
+  int rows, cols, out_c;
+  xenos_dtype dtype;            /* of x, residual and out */
+  const void* d_x;
+  long long x_stride;
+  const float* d_gamma;
+  float eps;
+  const void* d_w;
+  const float* d_w_scale;
+  const float* d_bias;
+  const void* d_residual;
+  long long residual_stride;
+  int relu;
+  void* d_out;
+  long long out_stride;
+} xenos_linear_args;
+xenos_status xenos_linear_workspace(int rows, int cols, size_t* bytes);
+xenos_status xenos_linear(const xenos_linear_args* args, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
 /* A cache of keys and values in 8-bit integers, quantised row by row (one token's head_dim values of one head) like xenos_quant_rows, in pages of
  * page_tokens tokens that a caller deals out to its sequences in any order.  A token's slot is page * page_tokens + its place in the page.  Memory,
  * all of it the caller's, in the order in which the attention's matrix instructions read it:

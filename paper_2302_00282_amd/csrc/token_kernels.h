@@ -18,6 +18,7 @@ struct QuantRowsArgs {
   long long stride, pitch;
   int rows, cols;
   float eps;
+  int vec;                                                   // rows of x start at 16-byte boundaries
 };
 int launch_quant_rows(const QuantRowsArgs& a, int dtype, void* stream);
 
@@ -32,6 +33,9 @@ struct QuantMatmulArgs {
   int vec_out;                                               // rows of out and res start at multiples of four elements, whole fours are stored at once
 };
 int launch_quant_matmul(const QuantMatmulArgs& a, int dtype, void* stream);
+// Both for one layer.  A few short rows are quantised by every workgroup of the product for itself, which saves a launch; r.q and r.scale are not used then.
+inline bool linear_in_one(int rows, long long pitch) { return rows <= 16 && rows * pitch <= 8192; }
+int launch_linear(const QuantRowsArgs& r, const QuantMatmulArgs& a, int dtype, void* stream);
 
 struct CacheArgs {
   int8_t *k, *v;                                             // 16-byte aligned, as the scales are; the layouts of xenos.h

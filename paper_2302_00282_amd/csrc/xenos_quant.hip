@@ -5,9 +5,9 @@
 namespace xenos {
 
 // Eight values of a row from element i on, those behind the row's end as zeros.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* row, int i, int cols, float* f) {
-  if (VEC && i + 8 <= cols) {
+template <typename T>
+__device__ __forceinline__ void load8(const T* row, int i, int cols, int vec, float* f) {
+  if (vec && i + 8 <= cols) {
 #pragma unroll
     for (int c = 0; c < 8 / Tr<T>::CE; ++c) Tr<T>::unpack(*(const u32x4_t*)(row + i + c * Tr<T>::CE), f + c * Tr<T>::CE);
   } else {
@@ -15,10 +15,23 @@ __device__ __forceinline__ void load8(const T* row, int i, int cols, float* f) {
     for (int e = 0; e < 8; ++e) f[e] = i + e < cols ? Tr<T>::ld(row, i + e) : 0.f;
   }
 }
+__device__ __forceinline__ void times_gamma(const QuantRowsArgs& a, int i, const float* f, float* v) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = a.gamma ? f[e] * (i + e < a.cols ? a.gamma[i + e] : 0.f) : f[e];
+}
+__device__ __forceinline__ uint2 packed8(const RowStep& step, const float* v) {
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w[e >> 2] |= ((uint32_t)step(v[e]) & 0xffu) << (8 * (e & 3));
+  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ float row_scale(const QuantRowsArgs& a, const RowStep& step, float sq) {
+  return a.gamma ? step.scale() * (1.f / sqrtf(sq / (float)a.cols + a.eps)) : step.scale();
+}
 
 // One workgroup per row: q = rint(x g 127 / a), a = max|x g|, scale = a / 127 [/ rms(x)].  The norm's factor is one number per row: it
 // cancels in q, so that the rounded values do not depend on how the squares are summed.  Two passes over the row, the second from the cache.
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(1024) void quant_rows_kernel(QuantRowsArgs a) {
   __shared__ uint32_t s_max[16];
   __shared__ float s_sum[16];
@@ -29,13 +42,11 @@ __global__ __launch_bounds__(1024) void quant_rows_kernel(QuantRowsArgs a) {
     uint32_t m = 0;
     float sq = 0.f;
     for (int i = (int)threadIdx.x * 8; i < a.cols; i += step) {
-      float f[8];
-      load8<T, VEC>(row, i, a.cols, f);
-  #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        sq += f[e] * f[e];
-        m = umax(m, magnitude(a.gamma ? f[e] * (i + e < a.cols ? a.gamma[i + e] : 0.f) : f[e]));
-      }
+      float f[8], v[8];
+      load8<T>(row, i, a.cols, a.vec, f);
+      times_gamma(a, i, f, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sq += f[e] * f[e], m = umax(m, magnitude(v[e]));
     }
     m = wave_max(m);
     sq = wave_sum(sq);
@@ -43,30 +54,22 @@ __global__ __launch_bounds__(1024) void quant_rows_kernel(QuantRowsArgs a) {
     __syncthreads();
     m = 0, sq = 0.f;
     for (int w = 0; w < waves; ++w) { m = umax(m, s_max[w]); sq += s_sum[w]; }
-    const RowStep step8(m);
+    const RowStep unit(m);
     for (int i = (int)threadIdx.x * 8; i < (int)a.pitch; i += step) {
-      float f[8];
-      load8<T, VEC>(row, i, a.cols, f);
-      uint32_t w[2] = {0, 0};
-  #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float v = a.gamma ? f[e] * (i + e < a.cols ? a.gamma[i + e] : 0.f) : f[e];
-        w[e >> 2] |= ((uint32_t)step8(v) & 0xffu) << (8 * (e & 3));
-      }
-      *(uint2*)(q + i) = make_uint2(w[0], w[1]);
+      float f[8], v[8];
+      load8<T>(row, i, a.cols, a.vec, f);
+      times_gamma(a, i, f, v);
+      *(uint2*)(q + i) = packed8(unit, v);
     }
-    if (threadIdx.x == 0) a.scale[at] = a.gamma ? step8.scale() * (1.f / sqrtf(sq / (float)a.cols + a.eps)) : step8.scale();
-    __syncthreads();                                            // (s_max and s_sum are free again)
+    if (threadIdx.x == 0) a.scale[at] = row_scale(a, unit, sq);
+    __syncthreads();                                          // (s_max and s_sum are free again)
   }
 }
 
 template <typename T>
 static int quant_rows(const QuantRowsArgs& a, hipStream_t st) {
-  const int esz = (int)sizeof(T);
-  const bool vec = (uintptr_t)a.x % 16 == 0 && a.stride * esz % 16 == 0;
   const int threads = a.pitch <= 2048 ? 256 : 1024, grid = a.rows < 65536 ? a.rows : 65536;
-  if (vec) quant_rows_kernel<T, true><<<grid, threads, 0, st>>>(a);
-  else quant_rows_kernel<T, false><<<grid, threads, 0, st>>>(a);
+  quant_rows_kernel<T><<<grid, threads, 0, st>>>(a);
   return (int)hipGetLastError();
 }
 int launch_quant_rows(const QuantRowsArgs& a, int dtype, void* stream) {
@@ -75,9 +78,8 @@ int launch_quant_rows(const QuantRowsArgs& a, int dtype, void* stream) {
 
 // y = act(acc xs ws + bias + residual) for four neighbouring columns n of row m.
 template <typename T>
-__device__ __forceinline__ void store4(const QuantMatmulArgs& a, int m, int n, const i32x4_t& acc) {
+__device__ __forceinline__ void store4(const QuantMatmulArgs& a, int m, int n, const i32x4_t& acc, float xs) {
   if (m >= a.M || n >= a.N) return;
-  const float xs = a.xs[m];
   T* out = (T*)a.out + (long long)m * a.out_stride + n;
   const T* res = a.res ? (const T*)a.res + (long long)m * a.res_stride + n : nullptr;
   const bool whole = a.vec_out && n + 4 <= a.N;
@@ -110,22 +112,67 @@ __device__ __forceinline__ void store4(const QuantMatmulArgs& a, int m, int n, c
   }
 }
 
-// Few rows: the weights are the work.  A workgroup has 16 output channels and all of K, which its wavefronts share; every fragment goes
+// The rows of x that a workgroup of eight wavefronts multiplies, quantised by itself into LDS (`pitch` bytes a row) as quant_rows_kernel does: eight, four, two wavefronts
+// or one to a row.
+template <typename T>
+__device__ __forceinline__ void quant_into_lds(const QuantRowsArgs& a, int8_t* q, float* scale) {
+  __shared__ uint32_t s_max[16];
+  __shared__ float s_sum[16][8];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, share = a.rows > 4 ? 1 : a.rows > 2 ? 2 : a.rows > 1 ? 4 : 8, piece = wave % share;
+  if (threadIdx.x < 16) s_max[threadIdx.x] = 0;
+  __syncthreads();
+  for (int r = wave / share; r < a.rows; r += 8 / share) {
+    const T* row = (const T*)a.x + r * a.stride;
+    uint32_t m = 0;
+    float sq = 0.f;
+    for (int i = (piece * 64 + lane) * 8; i < a.cols; i += share * 512) {
+      float f[8], v[8];
+      load8<T>(row, i, a.cols, a.vec, f);
+      times_gamma(a, i, f, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sq += f[e] * f[e], m = umax(m, magnitude(v[e]));
+    }
+    m = wave_max(m);
+    sq = wave_sum(sq);
+    if (lane == 0) atomicMax(&s_max[r], m), s_sum[r][piece] = sq;
+  }
+  __syncthreads();
+  for (int r = wave / share; r < a.rows; r += 8 / share) {
+    const T* row = (const T*)a.x + r * a.stride;
+    const RowStep step(s_max[r]);
+    for (int i = (piece * 64 + lane) * 8; i < (int)a.pitch; i += share * 512) {
+      float f[8], v[8];
+      load8<T>(row, i, a.cols, a.vec, f);
+      times_gamma(a, i, f, v);
+      *(uint2*)(q + r * a.pitch + i) = packed8(step, v);
+    }
+    if (piece == 0 && lane == 0) {
+      float sq = 0.f;
+      for (int w = 0; w < share; ++w) sq += s_sum[r][w];
+      scale[r] = row_scale(a, step, sq);
+    }
+  }
+  __syncthreads();
+}
+
+// Few rows: the weights are the work.  A workgroup has 16 output channels and all of K, which its wavefronts share; every fragment of the weights goes
 // from memory to registers, a lane's 16 bytes of one weight row at a time, and the sums (whole numbers: exact in any order) meet in LDS.
-template <typename T, int MT>
-__global__ __launch_bounds__(512) void quant_matvec_kernel(QuantMatmulArgs a) {
+// OWN: x comes as it is, and every workgroup quantises all of it for itself.
+template <typename T, int MT, bool OWN>
+__global__ __launch_bounds__(512) void quant_matvec_kernel(QuantMatmulArgs a, QuantRowsArgs qa) {
   __shared__ i32x4_t part[8][MT][64];
+  extern __shared__ __attribute__((aligned(16))) int8_t s_q[];
+  __shared__ float s_scale[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  const int n0 = (int)blockIdx.x * 16;
+  const int n0 = (int)blockIdx.x * 16, pitch = (int)a.pitch;
   const int8_t* w = a.w + (long long)(n0 + r < a.N ? n0 + r : a.N - 1) * a.pitch + g * 16;
+  if (OWN) quant_into_lds<T>(qa, s_q, s_scale);
   const int8_t* x[MT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) x[t] = a.x + (long long)(16 * t + r < a.M ? 16 * t + r : a.M - 1) * a.pitch + g * 16;
+  for (int t = 0; t < MT; ++t) x[t] = (OWN ? s_q : a.x) + (16 * t + r < a.M ? 16 * t + r : a.M - 1) * a.pitch + g * 16;
   i32x4_t acc[MT] = {};
-  const int steps = (int)(a.pitch / 128);
 #pragma unroll 4
-  for (int s = wave; s < steps; s += 8) {
-    const long long k = (long long)s * 128;
+  for (int k = wave * 128; k < pitch; k += 1024) {
     const i32x4_t w0 = *(const i32x4_t*)(w + k), w1 = *(const i32x4_t*)(w + k + 64);
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
@@ -140,7 +187,8 @@ __global__ __launch_bounds__(512) void quant_matvec_kernel(QuantMatmulArgs a) {
     i32x4_t sum = part[0][t][lane];
 #pragma unroll
     for (int v = 1; v < 8; ++v) sum += part[v][t][lane];
-    store4<T>(a, 16 * t + r, n0 + 4 * g, sum);
+    const int m = 16 * t + r;
+    store4<T>(a, m, n0 + 4 * g, sum, OWN ? s_scale[m < 16 ? m : 0] : m < a.M ? a.xs[m] : 0.f);
   }
 }
 
@@ -185,22 +233,37 @@ __global__ __launch_bounds__(256) void quant_matmul_kernel(QuantMatmulArgs a) {
     }
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < 4; ++j) {
+    const int m = m0 + wm + 16 * j + r;
+    const float xs = m < a.M ? a.xs[m] : 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) store4<T>(a, m0 + wm + 16 * j + r, n0 + wn + 16 * i + 4 * g, acc[i][j]);
+    for (int i = 0; i < 4; ++i) store4<T>(a, m, n0 + wn + 16 * i + 4 * g, acc[i][j], xs);
+  }
 }
 
 template <typename T>
 static int quant_matmul(const QuantMatmulArgs& a, hipStream_t st) {
   const int nt = (a.N + 15) / 16;
-  if (a.M <= 16) quant_matvec_kernel<T, 1><<<nt, 512, 0, st>>>(a);
-  else if (a.M <= 32) quant_matvec_kernel<T, 2><<<nt, 512, 0, st>>>(a);
-  else if (a.M <= 64) quant_matvec_kernel<T, 4><<<nt, 512, 0, st>>>(a);
+  const QuantRowsArgs none{};
+  if (a.M <= 16) quant_matvec_kernel<T, 1, false><<<nt, 512, 0, st>>>(a, none);
+  else if (a.M <= 32) quant_matvec_kernel<T, 2, false><<<nt, 512, 0, st>>>(a, none);
+  else if (a.M <= 64) quant_matvec_kernel<T, 4, false><<<nt, 512, 0, st>>>(a, none);
   else quant_matmul_kernel<T><<<(a.N + 127) / 128 * ((a.M + 127) / 128), 256, 0, st>>>(a);
   return (int)hipGetLastError();
 }
 int launch_quant_matmul(const QuantMatmulArgs& a, int dtype, void* stream) {
   return dtype ? quant_matmul<bf16_t>(a, (hipStream_t)stream) : quant_matmul<float>(a, (hipStream_t)stream);
+}
+
+int launch_linear(const QuantRowsArgs& r, const QuantMatmulArgs& a, int dtype, void* stream) {
+  if (linear_in_one(a.M, a.pitch)) {
+    const int nt = (a.N + 15) / 16, lds = a.M * (int)a.pitch;
+    if (dtype) quant_matvec_kernel<bf16_t, 1, true><<<nt, 512, lds, (hipStream_t)stream>>>(a, r);
+    else quant_matvec_kernel<float, 1, true><<<nt, 512, lds, (hipStream_t)stream>>>(a, r);
+    return (int)hipGetLastError();
+  }
+  const int err = launch_quant_rows(r, dtype, stream);
+  return err ? err : launch_quant_matmul(a, dtype, stream);
 }
 
 }  // namespace xenos

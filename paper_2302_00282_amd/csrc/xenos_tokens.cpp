@@ -20,6 +20,40 @@ xenos_status launched(int err, const char* what) {
   return err ? fail(XENOS_EDEVICE, "%s: %s", what, hipGetErrorString((hipError_t)err)) : XENOS_OK;
 }
 
+xenos_status rows_of(const char* who, const void* d_x, xenos_dtype dtype, int rows, int cols, long long row_stride, const float* d_gamma, float eps, void* d_q, float* d_scale,
+                     QuantRowsArgs& a) {
+  if (rows < 0 || cols <= 0 || !known(dtype)) return fail(XENOS_EINVAL, "%s: %d rows of %d columns, type %d", who, rows, cols, (int)dtype);
+  if (cols > XENOS_QUANT_MAX_COLS) return fail(XENOS_EUNSUPPORTED, "%s: %d columns, at most %d", who, cols, XENOS_QUANT_MAX_COLS);
+  if (rows == 0) return XENOS_OK;
+  if (!d_x || !d_q || !d_scale) return fail(XENOS_EINVAL, "%s: NULL argument", who);
+  if (rows > 1 && row_stride < cols) return fail(XENOS_ESHAPE, "%s: rows of %d elements, %lld apart", who, cols, row_stride);
+  if (!aligned(d_x, size_of(dtype)) || !aligned(d_gamma, 4) || !aligned(d_q, 16) || !aligned(d_scale, 4))
+    return fail(XENOS_EINVAL, "%s: a buffer is not aligned (the quantised rows, or the workspace: to 16 bytes)", who);
+  if (d_gamma && !(eps >= 0.f)) return fail(XENOS_EINVAL, "%s: eps %g", who, (double)eps);
+  a = QuantRowsArgs{d_x, d_gamma, (int8_t*)d_q, d_scale, rows > 1 ? row_stride : 0, quant_pitch(cols), rows, cols, eps, 0};
+  a.vec = aligned(d_x, 16) && a.stride * size_of(dtype) % 16 == 0;
+  return XENOS_OK;
+}
+
+xenos_status matmul_of(const char* who, const xenos_quant_matmul_args* p, QuantMatmulArgs& a) {
+  if (!p || p->rows < 0 || p->cols <= 0 || p->out_c < 0 || !known(p->dtype)) return fail(XENOS_EINVAL, "%s: bad argument", who);
+  if (p->cols > XENOS_QUANT_MAX_COLS) return fail(XENOS_EUNSUPPORTED, "%s: %d columns, at most %d", who, p->cols, XENOS_QUANT_MAX_COLS);
+  if (p->rows == 0 || p->out_c == 0) return XENOS_OK;
+  if (!p->d_q || !p->d_scale || !p->d_w || !p->d_w_scale || !p->d_out) return fail(XENOS_EINVAL, "%s: NULL argument", who);
+  if (p->rows > 1 && (p->out_stride < p->out_c || (p->d_residual && p->residual_stride < p->out_c)))
+    return fail(XENOS_ESHAPE, "%s: rows of %d elements, %lld (out) and %lld (residual) apart", who, p->out_c, p->out_stride, p->residual_stride);
+  const size_t esz = size_of(p->dtype);
+  if (!aligned(p->d_q, 16) || !aligned(p->d_w, 16) || !aligned(p->d_scale, 4) || !aligned(p->d_w_scale, 4) || !aligned(p->d_bias, 4) || !aligned(p->d_out, esz) ||
+      !aligned(p->d_residual, esz))
+    return fail(XENOS_EINVAL, "%s: a buffer is not aligned (quantised rows: to 16 bytes)", who);
+  if (((p->rows + 63ll) / 64) * ((p->out_c + 15ll) / 16) > kMostGroups)
+    return fail(XENOS_EUNSUPPORTED, "%s: %d x %d results are more than one launch holds", who, p->rows, p->out_c);
+  a = QuantMatmulArgs{(const int8_t*)p->d_q, (const int8_t*)p->d_w, p->d_scale, p->d_w_scale, p->d_bias, p->d_residual, p->d_out, quant_pitch(p->cols),
+                      p->rows > 1 ? p->residual_stride : 0, p->rows > 1 ? p->out_stride : 0, p->rows, p->out_c, p->relu ? 1 : 0, 0};
+  a.vec_out = a.out_stride % 4 == 0 && aligned(a.out, 4 * esz) && (!a.res || (a.res_stride % 4 == 0 && aligned(a.res, 4 * esz)));
+  return XENOS_OK;
+}
+
 xenos_status cache_of(const xenos_cache* c, const char* who, CacheArgs& a) {
   if (!c || c->n_pages < 0 || c->page_tokens <= 0 || c->heads <= 0 || c->head_dim <= 0) return fail(XENOS_EINVAL, "%s: bad cache description", who);
   if (c->page_tokens % 16 || c->head_dim % 16 || c->head_dim > 256)
@@ -59,35 +93,41 @@ extern "C" {
 
 xenos_status xenos_quant_rows(const void* d_x, xenos_dtype dtype, int rows, int cols, long long row_stride, const float* d_gamma, float eps,
                               void* d_q, float* d_scale, void* hip_stream) {
-  if (rows < 0 || cols <= 0 || !known(dtype)) return fail(XENOS_EINVAL, "xenos_quant_rows: %d rows of %d columns, type %d", rows, cols, (int)dtype);
-  if (cols > XENOS_QUANT_MAX_COLS) return fail(XENOS_EUNSUPPORTED, "xenos_quant_rows: %d columns, at most %d", cols, XENOS_QUANT_MAX_COLS);
-  if (rows == 0) return XENOS_OK;
-  if (!d_x || !d_q || !d_scale) return fail(XENOS_EINVAL, "xenos_quant_rows: NULL argument");
-  if (rows > 1 && row_stride < cols) return fail(XENOS_ESHAPE, "xenos_quant_rows: rows of %d elements, %lld apart", cols, row_stride);
-  if (!aligned(d_x, size_of(dtype)) || !aligned(d_gamma, 4) || !aligned(d_q, 16) || !aligned(d_scale, 4))
-    return fail(XENOS_EINVAL, "xenos_quant_rows: a buffer is not aligned (the quantised rows: to 16 bytes)");
-  if (d_gamma && !(eps >= 0.f)) return fail(XENOS_EINVAL, "xenos_quant_rows: eps %g", (double)eps);
-  QuantRowsArgs a{d_x, d_gamma, (int8_t*)d_q, d_scale, rows > 1 ? row_stride : 0, quant_pitch(cols), rows, cols, eps};
+  QuantRowsArgs a{};
+  const xenos_status rc = rows_of("xenos_quant_rows", d_x, dtype, rows, cols, row_stride, d_gamma, eps, d_q, d_scale, a);
+  if (rc != XENOS_OK || rows == 0) return rc;
   return launched(launch_quant_rows(a, dtype, hip_stream), "xenos_quant_rows");
 }
 
 xenos_status xenos_quant_matmul(const xenos_quant_matmul_args* p, void* hip_stream) {
-  if (!p || p->rows < 0 || p->cols <= 0 || p->out_c < 0 || !known(p->dtype)) return fail(XENOS_EINVAL, "xenos_quant_matmul: bad argument");
-  if (p->cols > XENOS_QUANT_MAX_COLS) return fail(XENOS_EUNSUPPORTED, "xenos_quant_matmul: %d columns, at most %d", p->cols, XENOS_QUANT_MAX_COLS);
-  if (p->rows == 0 || p->out_c == 0) return XENOS_OK;
-  if (!p->d_q || !p->d_scale || !p->d_w || !p->d_w_scale || !p->d_out) return fail(XENOS_EINVAL, "xenos_quant_matmul: NULL argument");
-  if (p->rows > 1 && (p->out_stride < p->out_c || (p->d_residual && p->residual_stride < p->out_c)))
-    return fail(XENOS_ESHAPE, "xenos_quant_matmul: rows of %d elements, %lld (out) and %lld (residual) apart", p->out_c, p->out_stride, p->residual_stride);
-  const size_t esz = size_of(p->dtype);
-  if (!aligned(p->d_q, 16) || !aligned(p->d_w, 16) || !aligned(p->d_scale, 4) || !aligned(p->d_w_scale, 4) || !aligned(p->d_bias, 4) || !aligned(p->d_out, esz) ||
-      !aligned(p->d_residual, esz))
-    return fail(XENOS_EINVAL, "xenos_quant_matmul: a buffer is not aligned (quantised rows: to 16 bytes)");
-  if (((p->rows + 63ll) / 64) * ((p->out_c + 15ll) / 16) > kMostGroups)
-    return fail(XENOS_EUNSUPPORTED, "xenos_quant_matmul: %d x %d results are more than one launch holds", p->rows, p->out_c);
-  QuantMatmulArgs a{(const int8_t*)p->d_q, (const int8_t*)p->d_w, p->d_scale, p->d_w_scale, p->d_bias, p->d_residual, p->d_out, quant_pitch(p->cols),
-                    p->rows > 1 ? p->residual_stride : 0, p->rows > 1 ? p->out_stride : 0, p->rows, p->out_c, p->relu ? 1 : 0, 0};
-  a.vec_out = a.out_stride % 4 == 0 && aligned(a.out, 4 * esz) && (!a.res || (a.res_stride % 4 == 0 && aligned(a.res, 4 * esz)));
+  QuantMatmulArgs a{};
+  const xenos_status rc = matmul_of("xenos_quant_matmul", p, a);
+  if (rc != XENOS_OK || p->rows == 0 || p->out_c == 0) return rc;
   return launched(launch_quant_matmul(a, p->dtype, hip_stream), "xenos_quant_matmul");
+}
+
+xenos_status xenos_linear_workspace(int rows, int cols, size_t* bytes) {
+  if (rows < 0 || cols <= 0 || cols > XENOS_QUANT_MAX_COLS || !bytes) return fail(XENOS_EINVAL, "xenos_linear_workspace: %d rows of %d columns", rows, cols);
+  *bytes = linear_in_one(rows, quant_pitch(cols)) ? 0 : (size_t)rows * (quant_pitch(cols) + 4);
+  return XENOS_OK;
+}
+
+xenos_status xenos_linear(const xenos_linear_args* p, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!p) return fail(XENOS_EINVAL, "xenos_linear: NULL argument");
+  size_t need = 0;
+  if (p->rows >= 0 && p->cols > 0 && p->cols <= XENOS_QUANT_MAX_COLS) xenos_linear_workspace(p->rows, p->cols, &need);
+  if (need && (!d_workspace || workspace_bytes < need)) return fail(XENOS_EINVAL, "xenos_linear: a workspace of %zu bytes, %zu are needed", workspace_bytes, need);
+  // (where nothing is stored there, any aligned address will do)
+  int8_t* q = need ? (int8_t*)d_workspace : (int8_t*)16;
+  float* scale = need ? (float*)(q + p->rows * quant_pitch(p->cols)) : (float*)16;
+  QuantRowsArgs r{};
+  xenos_status rc = rows_of("xenos_linear", p->d_x, p->dtype, p->rows, p->cols, p->x_stride, p->d_gamma, p->eps, q, scale, r);
+  if (rc != XENOS_OK) return rc;
+  const xenos_quant_matmul_args m{p->rows, p->cols, p->out_c, q, scale, p->d_w, p->d_w_scale, p->d_bias, p->d_residual, p->residual_stride, p->relu, p->dtype, p->d_out, p->out_stride};
+  QuantMatmulArgs a{};
+  rc = matmul_of("xenos_linear", &m, a);
+  if (rc != XENOS_OK || p->rows == 0 || p->out_c == 0) return rc;
+  return launched(launch_linear(r, a, p->dtype, hip_stream), "xenos_linear");
 }
 
 xenos_status xenos_cache_write(const xenos_cache* cache, int n_tokens, const void* d_k, long long k_token_stride, long long k_head_stride,

@@ -60,6 +60,12 @@ class QuantMatmulArgs(C.Structure):
                 ("relu", C.c_int), ("dtype", C.c_int), ("d_out", C.c_void_p), ("out_stride", C.c_longlong)]
 
 
+class LinearArgs(C.Structure):
+    _fields_ = [("rows", C.c_int), ("cols", C.c_int), ("out_c", C.c_int), ("dtype", C.c_int), ("d_x", C.c_void_p), ("x_stride", C.c_longlong),
+                ("d_gamma", C.c_void_p), ("eps", C.c_float), ("d_w", C.c_void_p), ("d_w_scale", C.c_void_p), ("d_bias", C.c_void_p),
+                ("d_residual", C.c_void_p), ("residual_stride", C.c_longlong), ("relu", C.c_int), ("d_out", C.c_void_p), ("out_stride", C.c_longlong)]
+
+
 class Cache(C.Structure):
     _fields_ = [("n_pages", C.c_int), ("page_tokens", C.c_int), ("heads", C.c_int), ("head_dim", C.c_int),
                 ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p)]
@@ -110,6 +116,8 @@ def lib():
         L.xenos_probe_read.argtypes = [C.POINTER(HwInfo), vp, C.c_size_t, vp, C.c_size_t, vp]
         L.xenos_quant_rows.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_longlong, vp, C.c_float, vp, vp, vp]
         L.xenos_quant_matmul.argtypes = [C.POINTER(QuantMatmulArgs), vp]
+        L.xenos_linear_workspace.argtypes = [C.c_int, C.c_int, C.POINTER(C.c_size_t)]
+        L.xenos_linear.argtypes = [C.POINTER(LinearArgs), vp, C.c_size_t, vp]
         L.xenos_cache_write.argtypes = [C.POINTER(Cache), C.c_int, vp, C.c_longlong, C.c_longlong, vp, C.c_longlong, C.c_longlong, C.c_int, vp, vp]
         L.xenos_cache_read.argtypes = [C.POINTER(Cache), C.c_int, vp, vp, vp, C.c_int, vp]
         L.xenos_logprobs_workspace.argtypes = [C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
@@ -122,6 +130,7 @@ def lib():
         for f in ("xenos_graph_create", "xenos_plan_link_split", "xenos_plan_query", "xenos_plan_bind",
                   "xenos_run", "xenos_run_graph", "xenos_run_static", "xenos_run_with", "xenos_run_chain", "xenos_plan_tune",
                   "xenos_probe_mfma", "xenos_probe_read", "xenos_quant_rows", "xenos_quant_matmul",
+                  "xenos_linear_workspace", "xenos_linear",
                   "xenos_cache_write", "xenos_cache_read", "xenos_logprobs_workspace", "xenos_logprobs",
                   "xenos_attention_workspace", "xenos_attention"):
             getattr(L, f).restype = C.c_int
@@ -227,6 +236,16 @@ def xenos_quant_matmul(args: QuantMatmulArgs, stream: int = 0):
     _check(lib().xenos_quant_matmul(C.byref(args), stream))
 
 
+def xenos_linear_workspace(rows: int, cols: int) -> int:
+    n = C.c_size_t()
+    _check(lib().xenos_linear_workspace(rows, cols, C.byref(n)))
+    return n.value
+
+
+def xenos_linear(args: LinearArgs, d_workspace: int = 0, workspace_bytes: int = 0, stream: int = 0):
+    _check(lib().xenos_linear(C.byref(args), d_workspace, workspace_bytes, stream))
+
+
 def xenos_cache_write(cache: Cache, n_tokens: int, d_k: int, k_token_stride: int, k_head_stride: int, d_v: int, v_token_stride: int, v_head_stride: int,
                       dtype: int, d_slots: int, stream: int = 0):
     _check(lib().xenos_cache_write(C.byref(cache), n_tokens, d_k, k_token_stride, k_head_stride, d_v, v_token_stride, v_head_stride, dtype, d_slots, stream))
@@ -246,7 +265,7 @@ def xenos_attention(cache: Cache, args: AttentionArgs, d_workspace: int = 0, wor
     _check(lib().xenos_attention(C.byref(cache), C.byref(args), d_workspace, workspace_bytes, stream))
 
 
-XENOS_TOP_MAX = 64
+XENOS_TOP_MAX, XENOS_QUANT_MAX_COLS = 64, 131072
 
 
 def xenos_logprobs_workspace(rows: int, vocab: int, top: int) -> int:

@@ -182,3 +182,58 @@ def test_c_entries_refuse_before_any_launch():
         assert e.value.status == status and "xenos_quant_matmul" in str(e.value)
     X.xenos_quant_matmul(X.QuantMatmulArgs(**dict(product, rows=0, d_q=None)))
     X.xenos_quant_matmul(X.QuantMatmulArgs(**dict(product, out_c=0, d_out=None)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("extras", ["", "bias residual relu"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols,out_c", [(1, 1, 1), (1, 512, 2048), (1, 8192, 24), (1, 8193, 24), (2, 1001, 130), (3, 2500, 40), (5, 1500, 33), (8, 1024, 48), (16, 512, 100), (16, 500, 17),
+                                             (17, 300, 20), (40, 1000, 64), (200, 640, 200)])
+def test_linear_is_its_two_steps(rows, cols, out_c, dtype, extras):
+    x = drawn(rows, cols, dtype, 1).cuda()
+    w, w_scale = T.quantize_rows(drawn(out_c, cols, torch.float32, 2).cuda())
+    more = dict(bias=drawn(1, out_c, torch.float32, 5)[0].cuda(), residual=drawn(rows, out_c, dtype, 6).cuda(), relu=True) if extras else {}
+    q, scale = T.quantize_rows(x)
+    assert torch.equal(T.linear(x, w, w_scale, **more), T.quant_matmul(q, scale, w, w_scale, cols, dtype=dtype, **more))
+    # behind a norm the squares may be summed in another order: the scale is off by as much twice, the whole numbers are the same
+    gamma = torch.rand(cols, generator=torch.Generator().manual_seed(1)) - 0.3
+    q, scale = T.quantize_rows(x, gamma.cuda())
+    want, size = product_by_definition(q, rows_by_definition(x.cpu(), gamma)[1].cuda(), w, w_scale, more.get("bias"), more.get("residual"), bool(extras))
+    bound = (5.1 + cols / 256 + 32) * U32 * size + (U16 * want.abs() if dtype == torch.bfloat16 else 0) * 1.01 + 1e-38
+    assert torch.all((T.linear(x, w, w_scale, gamma=gamma.cuda(), **more).double() - want).abs() <= bound)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_linear_of_rows_at_any_address_and_without_numbers(dtype):
+    w, w_scale = T.quantize_rows(drawn(40, 333, torch.float32, 2).cuda())
+    wide = drawn(9, 1000, dtype, 3).cuda()
+    for view in (wide[:, 1:334], wide[::2, :333], wide[:3, 8:341], wide[4:5, 3:336], wide.t()[:333].t()):
+        q, scale = T.quantize_rows(view)
+        assert torch.equal(T.linear(view, w, w_scale), T.quant_matmul(q, scale, w, w_scale, 333, dtype=dtype))
+    x = drawn(4, 333, dtype, 4)
+    x[0], x[1, 5], x[2, 332] = 0, float("nan"), float("-inf")
+    y = T.linear(x.cuda(), w, w_scale)
+    assert not y[0].any() and torch.isnan(y[1:3]).all() and torch.isfinite(y[3]).all()
+
+
+def test_linear_entries_refuse_before_any_launch():
+    p = 256
+    good = dict(rows=40, cols=1000, out_c=8, dtype=1, d_x=p, x_stride=1000, d_gamma=None, eps=1e-5, d_w=p, d_w_scale=p, d_bias=None, d_residual=None, residual_stride=0, relu=0, d_out=p, out_stride=8)
+    need = X.xenos_linear_workspace(40, 1000)
+    assert need == 40 * 1028 and X.xenos_linear_workspace(1, 1000) == 0 and X.xenos_linear_workspace(0, 5) == 0
+    for change, status in [(dict(rows=-1), X.XENOS_EINVAL), (dict(cols=0), X.XENOS_EINVAL), (dict(cols=1 << 18, x_stride=1 << 18), X.XENOS_EUNSUPPORTED), (dict(out_c=-1), X.XENOS_EINVAL),
+                           (dict(dtype=2), X.XENOS_EINVAL), (dict(d_x=None), X.XENOS_EINVAL), (dict(d_w=None), X.XENOS_EINVAL), (dict(d_out=None), X.XENOS_EINVAL), (dict(x_stride=999), X.XENOS_ESHAPE),
+                           (dict(out_stride=7), X.XENOS_ESHAPE), (dict(d_x=p + 1), X.XENOS_EINVAL), (dict(d_w=p + 8), X.XENOS_EINVAL), (dict(d_gamma=p, eps=-1.0), X.XENOS_EINVAL)]:
+        with pytest.raises(X.XenosError) as e:
+            X.xenos_linear(X.LinearArgs(**dict(good, **change)), p, 1 << 40)
+        assert e.value.status == status and "xenos_linear" in str(e.value), change
+    for ws, n in ((0, 0), (p, need - 1), (p + 8, 1 << 40)):
+        with pytest.raises(X.XenosError) as e:
+            X.xenos_linear(X.LinearArgs(**good), ws, n)
+        assert e.value.status == X.XENOS_EINVAL
+    for bad in ((-1, 5), (1, 0), (1, 131073)):
+        with pytest.raises(X.XenosError):
+            X.xenos_linear_workspace(*bad)
+    X.xenos_linear(X.LinearArgs(**dict(good, rows=0, d_x=None)))
+    X.xenos_linear(X.LinearArgs(**dict(good, out_c=0, d_out=None)), p, need)
