@@ -275,7 +275,7 @@ typedef struct {
   void* d_out;
   long long out_stride;
 } xenos_linear_args;
-xenos_status xenos_linear_workspace(int rows, int cols, size_t* bytes);
+xenos_status xenos_linear_workspace(int rows, int cols, int out_c, size_t* bytes);
 xenos_status xenos_linear(const xenos_linear_args* args, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
 /* A cache of keys and values in 8-bit integers, quantised row by row (one token's head_dim values of one head) like xenos_quant_rows, in pages of

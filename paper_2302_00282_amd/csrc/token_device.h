@@ -6,6 +6,7 @@
 namespace xenos {
 
 typedef __attribute__((ext_vector_type(4))) int i32x4_t;
+typedef __attribute__((ext_vector_type(16))) int i32x16_t;
 
 // The largest |value| by its bits: a NaN's are above infinity's, so that it stays.
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }

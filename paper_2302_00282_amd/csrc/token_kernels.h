@@ -18,7 +18,7 @@ struct QuantRowsArgs {
   long long stride, pitch;
   int rows, cols;
   float eps;
-  int vec;                                                   // rows of x start at 16-byte boundaries
+  int vec, vec_gamma;                                        // rows of x, and gamma, start at 16-byte boundaries
 };
 int launch_quant_rows(const QuantRowsArgs& a, int dtype, void* stream);
 
@@ -30,8 +30,11 @@ struct QuantMatmulArgs {
   long long pitch, res_stride, out_stride;
   int M, N;
   int relu;
-  int vec_out;                                               // rows of out and res start at multiples of four elements, whole fours are stored at once
+  int* part;                                                 // [quant_splits][M][part_pitch], 16-byte aligned, or null: K is not split
+  int part_pitch;                                            // N rounded up to eight
+  int vec_out;                                               // rows of out and res start at multiples of 16 bytes
 };
+int quant_splits(int rows, int out_c, long long pitch);
 int launch_quant_matmul(const QuantMatmulArgs& a, int dtype, void* stream);
 // Both for one layer.  A few short rows are quantised by every workgroup of the product for itself, which saves a launch; r.q and r.scale are not used then.
 inline bool linear_in_one(int rows, long long pitch) { return rows <= 16 && rows * pitch <= 8192; }

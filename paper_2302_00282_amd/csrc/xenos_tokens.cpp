@@ -30,7 +30,7 @@ xenos_status rows_of(const char* who, const void* d_x, xenos_dtype dtype, int ro
   if (!aligned(d_x, size_of(dtype)) || !aligned(d_gamma, 4) || !aligned(d_q, 16) || !aligned(d_scale, 4))
     return fail(XENOS_EINVAL, "%s: a buffer is not aligned (the quantised rows, or the workspace: to 16 bytes)", who);
   if (d_gamma && !(eps >= 0.f)) return fail(XENOS_EINVAL, "%s: eps %g", who, (double)eps);
-  a = QuantRowsArgs{d_x, d_gamma, (int8_t*)d_q, d_scale, rows > 1 ? row_stride : 0, quant_pitch(cols), rows, cols, eps, 0};
+  a = QuantRowsArgs{d_x, d_gamma, (int8_t*)d_q, d_scale, rows > 1 ? row_stride : 0, quant_pitch(cols), rows, cols, eps, 0, aligned(d_gamma, 16)};
   a.vec = aligned(d_x, 16) && a.stride * size_of(dtype) % 16 == 0;
   return XENOS_OK;
 }
@@ -49,9 +49,25 @@ xenos_status matmul_of(const char* who, const xenos_quant_matmul_args* p, QuantM
   if (((p->rows + 63ll) / 64) * ((p->out_c + 15ll) / 16) > kMostGroups)
     return fail(XENOS_EUNSUPPORTED, "%s: %d x %d results are more than one launch holds", who, p->rows, p->out_c);
   a = QuantMatmulArgs{(const int8_t*)p->d_q, (const int8_t*)p->d_w, p->d_scale, p->d_w_scale, p->d_bias, p->d_residual, p->d_out, quant_pitch(p->cols),
-                      p->rows > 1 ? p->residual_stride : 0, p->rows > 1 ? p->out_stride : 0, p->rows, p->out_c, p->relu ? 1 : 0, 0};
-  a.vec_out = a.out_stride % 4 == 0 && aligned(a.out, 4 * esz) && (!a.res || (a.res_stride % 4 == 0 && aligned(a.res, 4 * esz)));
+                      p->rows > 1 ? p->residual_stride : 0, p->rows > 1 ? p->out_stride : 0, p->rows, p->out_c, p->relu ? 1 : 0, nullptr, (p->out_c + 7) / 8 * 8, 0};
+  a.vec_out = a.out_stride * esz % 16 == 0 && aligned(a.out, 16) && (!a.res || (a.res_stride * esz % 16 == 0 && aligned(a.res, 16)));
   return XENOS_OK;
+}
+
+// A layer's workspace: quantised rows, their scales, and the sums of K's shares.
+struct LinearSpace {
+  size_t scale, part, bytes;
+  int splits;
+};
+LinearSpace linear_space(int rows, int cols, int out_c) {
+  const long long pitch = quant_pitch(cols);
+  LinearSpace s{};
+  if (rows == 0 || linear_in_one(rows, pitch)) return s;
+  s.scale = (size_t)rows * pitch;
+  s.part = (s.scale + (size_t)rows * 4 + 15) / 16 * 16;
+  s.splits = quant_splits(rows, out_c, pitch);
+  s.bytes = s.part + (s.splits > 1 ? (size_t)s.splits * rows * ((out_c + 7ll) / 8 * 8) * 4 : 0);
+  return s;
 }
 
 xenos_status cache_of(const xenos_cache* c, const char* who, CacheArgs& a) {
@@ -106,20 +122,20 @@ xenos_status xenos_quant_matmul(const xenos_quant_matmul_args* p, void* hip_stre
   return launched(launch_quant_matmul(a, p->dtype, hip_stream), "xenos_quant_matmul");
 }
 
-xenos_status xenos_linear_workspace(int rows, int cols, size_t* bytes) {
-  if (rows < 0 || cols <= 0 || cols > XENOS_QUANT_MAX_COLS || !bytes) return fail(XENOS_EINVAL, "xenos_linear_workspace: %d rows of %d columns", rows, cols);
-  *bytes = linear_in_one(rows, quant_pitch(cols)) ? 0 : (size_t)rows * (quant_pitch(cols) + 4);
+xenos_status xenos_linear_workspace(int rows, int cols, int out_c, size_t* bytes) {
+  if (rows < 0 || cols <= 0 || cols > XENOS_QUANT_MAX_COLS || out_c < 0 || !bytes) return fail(XENOS_EINVAL, "xenos_linear_workspace: %d rows of %d columns, %d results", rows, cols, out_c);
+  *bytes = linear_space(rows, cols, out_c).bytes;
   return XENOS_OK;
 }
 
 xenos_status xenos_linear(const xenos_linear_args* p, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
   if (!p) return fail(XENOS_EINVAL, "xenos_linear: NULL argument");
-  size_t need = 0;
-  if (p->rows >= 0 && p->cols > 0 && p->cols <= XENOS_QUANT_MAX_COLS) xenos_linear_workspace(p->rows, p->cols, &need);
-  if (need && (!d_workspace || workspace_bytes < need)) return fail(XENOS_EINVAL, "xenos_linear: a workspace of %zu bytes, %zu are needed", workspace_bytes, need);
+  LinearSpace space{};
+  if (p->rows >= 0 && p->cols > 0 && p->cols <= XENOS_QUANT_MAX_COLS && p->out_c >= 0) space = linear_space(p->rows, p->cols, p->out_c);
+  if (space.bytes && (!d_workspace || workspace_bytes < space.bytes)) return fail(XENOS_EINVAL, "xenos_linear: a workspace of %zu bytes, %zu are needed", workspace_bytes, space.bytes);
   // (where nothing is stored there, any aligned address will do)
-  int8_t* q = need ? (int8_t*)d_workspace : (int8_t*)16;
-  float* scale = need ? (float*)(q + p->rows * quant_pitch(p->cols)) : (float*)16;
+  int8_t* q = space.bytes ? (int8_t*)d_workspace : (int8_t*)16;
+  float* scale = space.bytes ? (float*)(q + space.scale) : (float*)16;
   QuantRowsArgs r{};
   xenos_status rc = rows_of("xenos_linear", p->d_x, p->dtype, p->rows, p->cols, p->x_stride, p->d_gamma, p->eps, q, scale, r);
   if (rc != XENOS_OK) return rc;
@@ -127,6 +143,7 @@ xenos_status xenos_linear(const xenos_linear_args* p, void* d_workspace, size_t 
   QuantMatmulArgs a{};
   rc = matmul_of("xenos_linear", &m, a);
   if (rc != XENOS_OK || p->rows == 0 || p->out_c == 0) return rc;
+  if (space.splits > 1) a.part = (int*)(q + space.part);
   return launched(launch_linear(r, a, p->dtype, hip_stream), "xenos_linear");
 }
 

@@ -132,7 +132,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, bias: Opt
     x, residual, rows = _rows(x), None if residual is None else _rows(residual), x.shape[0]
     w_scale, bias, gamma = _given(w_scale, "w_scale", device, (out_c,)), _given(bias, "bias", device, (out_c,)), _given(gamma, "gamma", device, (cols,))
     out = x.new_empty((rows, out_c))
-    need = X.xenos_linear_workspace(rows, cols) if cols <= X.XENOS_QUANT_MAX_COLS else 0
+    need = X.xenos_linear_workspace(rows, cols, out_c) if cols <= X.XENOS_QUANT_MAX_COLS else 0
     workspace = x.new_empty(need, dtype=torch.uint8) if need else None
     args = X.LinearArgs(rows, cols, out_c, _DTYPE[x.dtype], x.data_ptr(), x.stride(0), _address(gamma), eps, w.data_ptr(), w_scale.data_ptr(), _address(bias),
                         _address(residual), 0 if residual is None else residual.stride(0), relu, out.data_ptr(), out_c)

@@ -116,7 +116,7 @@ def lib():
         L.xenos_probe_read.argtypes = [C.POINTER(HwInfo), vp, C.c_size_t, vp, C.c_size_t, vp]
         L.xenos_quant_rows.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_longlong, vp, C.c_float, vp, vp, vp]
         L.xenos_quant_matmul.argtypes = [C.POINTER(QuantMatmulArgs), vp]
-        L.xenos_linear_workspace.argtypes = [C.c_int, C.c_int, C.POINTER(C.c_size_t)]
+        L.xenos_linear_workspace.argtypes = [C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
         L.xenos_linear.argtypes = [C.POINTER(LinearArgs), vp, C.c_size_t, vp]
         L.xenos_cache_write.argtypes = [C.POINTER(Cache), C.c_int, vp, C.c_longlong, C.c_longlong, vp, C.c_longlong, C.c_longlong, C.c_int, vp, vp]
         L.xenos_cache_read.argtypes = [C.POINTER(Cache), C.c_int, vp, vp, vp, C.c_int, vp]
@@ -236,9 +236,9 @@ def xenos_quant_matmul(args: QuantMatmulArgs, stream: int = 0):
     _check(lib().xenos_quant_matmul(C.byref(args), stream))
 
 
-def xenos_linear_workspace(rows: int, cols: int) -> int:
+def xenos_linear_workspace(rows: int, cols: int, out_c: int) -> int:
     n = C.c_size_t()
-    _check(lib().xenos_linear_workspace(rows, cols, C.byref(n)))
+    _check(lib().xenos_linear_workspace(rows, cols, out_c, C.byref(n)))
     return n.value
 
 

@@ -76,7 +76,7 @@ def product_by_definition(q, scale, w, w_scale, bias, residual, relu):
 @pytest.mark.parametrize("extras", ["", "bias", "residual", "bias residual relu", "relu"])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("rows,cols,out_c", [(1, 1, 1), (1, 512, 2048), (2, 129, 17), (16, 640, 100), (17, 1000, 1003), (33, 128, 48), (64, 2560, 30), (65, 300, 130),
-                                             (127, 1001, 257), (128, 512, 128), (300, 257, 515), (513, 1536, 1000), (1, 40000, 64), (260, 25088, 40)])
+                                             (127, 1001, 257), (128, 512, 128), (300, 257, 515), (513, 1536, 1000), (1, 40000, 64), (260, 25088, 40), (2000, 140, 2100), (4100, 130, 4200)])
 def test_product(rows, cols, out_c, dtype, extras):
     q, scale = T.quantize_rows(drawn(rows, cols, dtype, 1).cuda())
     w, w_scale = T.quantize_rows(drawn(out_c, cols, torch.float32, 2).cuda())
@@ -188,7 +188,8 @@ def test_c_entries_refuse_before_any_launch():
 @pytest.mark.parametrize("extras", ["", "bias residual relu"])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("rows,cols,out_c", [(1, 1, 1), (1, 512, 2048), (1, 8192, 24), (1, 8193, 24), (2, 1001, 130), (3, 2500, 40), (5, 1500, 33), (8, 1024, 48), (16, 512, 100), (16, 500, 17),
-                                             (17, 300, 20), (40, 1000, 64), (200, 640, 200)])
+                                             (17, 300, 20), (40, 1000, 64), (200, 640, 200), (33, 20001, 40), (70, 30000, 130), (300, 8192, 137), (5, 40000, 17),
+                                             (9, 600, 16400), (70, 200, 17000)])
 def test_linear_is_its_two_steps(rows, cols, out_c, dtype, extras):
     x = drawn(rows, cols, dtype, 1).cuda()
     w, w_scale = T.quantize_rows(drawn(out_c, cols, torch.float32, 2).cuda())
@@ -220,8 +221,9 @@ def test_linear_of_rows_at_any_address_and_without_numbers(dtype):
 def test_linear_entries_refuse_before_any_launch():
     p = 256
     good = dict(rows=40, cols=1000, out_c=8, dtype=1, d_x=p, x_stride=1000, d_gamma=None, eps=1e-5, d_w=p, d_w_scale=p, d_bias=None, d_residual=None, residual_stride=0, relu=0, d_out=p, out_stride=8)
-    need = X.xenos_linear_workspace(40, 1000)
-    assert need == 40 * 1028 and X.xenos_linear_workspace(1, 1000) == 0 and X.xenos_linear_workspace(0, 5) == 0
+    need = X.xenos_linear_workspace(40, 1000, 8)
+    assert need >= 40 * 1028 and X.xenos_linear_workspace(1, 1000, 8) == 0 and X.xenos_linear_workspace(0, 5, 8) == 0
+    assert X.xenos_linear_workspace(40, 20000, 64) >= 40 * 20096 + 160 + 2 * 40 * 64 * 4        # (K in shares)
     for change, status in [(dict(rows=-1), X.XENOS_EINVAL), (dict(cols=0), X.XENOS_EINVAL), (dict(cols=1 << 18, x_stride=1 << 18), X.XENOS_EUNSUPPORTED), (dict(out_c=-1), X.XENOS_EINVAL),
                            (dict(dtype=2), X.XENOS_EINVAL), (dict(d_x=None), X.XENOS_EINVAL), (dict(d_w=None), X.XENOS_EINVAL), (dict(d_out=None), X.XENOS_EINVAL), (dict(x_stride=999), X.XENOS_ESHAPE),
                            (dict(out_stride=7), X.XENOS_ESHAPE), (dict(d_x=p + 1), X.XENOS_EINVAL), (dict(d_w=p + 8), X.XENOS_EINVAL), (dict(d_gamma=p, eps=-1.0), X.XENOS_EINVAL)]:
@@ -232,7 +234,7 @@ def test_linear_entries_refuse_before_any_launch():
         with pytest.raises(X.XenosError) as e:
             X.xenos_linear(X.LinearArgs(**good), ws, n)
         assert e.value.status == X.XENOS_EINVAL
-    for bad in ((-1, 5), (1, 0), (1, 131073)):
+    for bad in ((-1, 5, 5), (1, 0, 5), (1, 131073, 5), (1, 5, -1)):
         with pytest.raises(X.XenosError):
             X.xenos_linear_workspace(*bad)
     X.xenos_linear(X.LinearArgs(**dict(good, rows=0, d_x=None)))
