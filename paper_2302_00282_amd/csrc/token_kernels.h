@@ -62,7 +62,7 @@ struct CacheReadArgs {
 struct AttentionShare {
   int tiles;                                                 // of rows
   int parts, part_len;                                       // pieces of the keys, of part_len (a multiple of 64) tokens each, the last one to the end
-  int whole;                                                 // the wavefronts of a workgroup have the same rows and take turns with the keys; else each has rows of its own
+  int row_tiles;                                             // 1, 2: the wavefronts of a workgroup have the same 16 or 32 rows and take turns with the keys; 0: 32 rows each
 };
 struct AttentionArgs {
   CacheArgs c;
@@ -70,11 +70,11 @@ struct AttentionArgs {
   uint16_t* out;
   long long q_token, q_head, out_token, out_head;
   const int *starts, *lengths, *tables, *prefix_table;
-  float* part;                                               // [row][slot](dim + 2 floats): unless there is one slot
+  float *part, *part_ml;                                     // [row][slot][dim] sums and [row][slot][2] maxima and normalisers, 16-byte aligned: unless there is one slot
   int n_seqs, n_queries, heads, group, table_stride, prefix_len;
   int vec_q, vec_out;                                        // rows of q are 16-byte, of out 8-byte aligned
   float scale2;                                              // scale log2 e
-  int row_tiles;                                             // of 16 rows, per wavefront: 1 or 2
+  int skip_prefix;                                           // this launch is the sequences' own keys alone
   AttentionShare own, prefix;
 };
 inline int attention_slots(const AttentionArgs& a) { return a.own.parts + a.prefix.parts; }

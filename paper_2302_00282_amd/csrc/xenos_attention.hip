@@ -15,7 +15,7 @@ namespace xenos {
 namespace {
 
 constexpr int kKeys = 64;                                     // of a step
-constexpr int kWaves = 4;
+constexpr int kWaves = 4, kMostParts = 64;                    // of a workgroup, of a segment
 
 // Eight bytes as bf16: whole numbers up to 127, exact.
 __device__ __forceinline__ bf16x8_t whole8(uint32_t lo, uint32_t hi) {
@@ -52,21 +52,22 @@ struct Item {
   int row0, rows;                                             // first row of the tile; rows of the item in all (queries times the group)
   int begin, end;                                             // keys
   int slot;
-  bool prefix, whole;
+  bool prefix;
 };
 
-__device__ __forceinline__ Item item_of(const AttentionArgs& a, int at, int waves_rows) {
+// The workgroup's item of a launch; its row tiles have tile_rows rows.  Heads change fastest (an XCD then reads the keys of few of them), and the last rows, which see
+// the most keys, come first.
+__device__ __forceinline__ Item item_of(const AttentionArgs& a, int at, int tile_rows) {
   Item it;
-  const int front = a.prefix.parts * a.prefix.tiles * a.c.heads;
+  const int front = a.skip_prefix ? 0 : a.prefix.parts * a.prefix.tiles * a.c.heads;
   it.prefix = at < front;
   const AttentionShare& s = it.prefix ? a.prefix : a.own;
   if (!it.prefix) at -= front;
-  const int tile = at % s.tiles;
-  at /= s.tiles;
   it.head = at % a.c.heads;
   at /= a.c.heads;
+  const int tile = s.tiles - 1 - at % s.tiles;
+  at /= s.tiles;
   const int part = at % s.parts, seq = at / s.parts;
-  it.whole = s.whole;
   if (it.prefix) {
     it.table = a.prefix_table, it.tokens = a.prefix_len, it.first_query = 0, it.queries = a.n_queries, it.slot = part;
   } else {
@@ -81,32 +82,47 @@ __device__ __forceinline__ Item item_of(const AttentionArgs& a, int at, int wave
   }
   if (a.c.n_pages == 0) it.tokens = 0;
   it.rows = it.queries * a.group;
-  it.row0 = tile * (it.whole ? waves_rows : kWaves * waves_rows);
+  it.row0 = tile * tile_rows;
   it.begin = part * s.part_len;
   it.end = part == s.parts - 1 || it.begin + s.part_len > it.tokens ? it.tokens : it.begin + s.part_len;
   return it;
 }
 
-// NB: blocks of 64 dimensions; MT: tiles of 16 rows per wavefront.
+// Where a block of 16 keys of a segment lies: its first row among the cache's, if it has a page.
+struct Block16 {
+  long long row;
+  bool ok;
+  __device__ __forceinline__ Block16(const AttentionArgs& a, const Item& it, int key, int page) {
+    ok = key < it.tokens && (unsigned)page < (unsigned)a.c.n_pages;
+    row = ok ? ((long long)page * a.c.heads + it.head) * a.c.page + key % a.c.page : 0;
+  }
+};
+
+// The reference m of a row's exponents follows the row's maximum only when that has grown by more than 2^kSlack: probabilities up to 2^kSlack are as exact, and
+// the exchange of maxima and the rescaling of O are rare.
+constexpr float kSlack = 8.f;
+
+// Few rows: the wavefronts of a workgroup have the same 16 MT rows and take turns with the keys; their states meet in LDS at the end.  NB: blocks of 64 dimensions.
 template <int NB, int MT>
-__global__ __launch_bounds__(64 * kWaves) void attention_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(64 * kWaves, MT == 1 && NB <= 2 ? 4 - NB : 1) void attention_kernel(AttentionArgs a) {
   constexpr int DT = 4 * NB, REC = MT * (4 * DT + 2);         // tiles of 16 dimensions; floats of a lane's state
   __shared__ float s_state[kWaves / 2][REC][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4, dim = a.c.dim;
+  __shared__ __attribute__((aligned(16))) float s_scale[kWaves][2][kKeys];
   Item it = item_of(a, (int)blockIdx.x, 16 * MT);
-  const AttentionShare& share = it.prefix ? a.prefix : a.own;
-  const int step_rows = share.tiles * (it.whole ? 16 * MT : kWaves * 16 * MT);
+  const int step_rows = (it.prefix ? a.prefix : a.own).tiles * 16 * MT;
   for (; it.row0 < it.rows; it.row0 += step_rows) {           // (once, unless a sequence has more queries than was said)
-    const int row_first = it.row0 + (it.whole ? 0 : wave * 16 * MT);
+    int lane = threadIdx.x & 63, dim = a.c.dim;
+    asm volatile("" : "+v"(lane), "+s"(dim));                 // (nothing is made before this loop, and kept in registers through it)
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     // rows of this lane: queries in bf16, and the keys they see
     bf16x8_t q[MT][NB][2];
-    int limit[MT], least = 0x7fffffff, most = 0;
+    int limit[MT], most = 0;
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-      const int row = row_first + 16 * t + r, query = row / a.group, h = it.head * a.group + row - query * a.group;
+      const int row = it.row0 + 16 * t + r, query = row / a.group, h = it.head * a.group + row - query * a.group;
       const bool ok = row < it.rows;
       limit[t] = !ok ? 0 : it.prefix ? it.tokens : it.tokens - it.queries + query + 1;
-      least = min(least, limit[t]), most = max(most, limit[t]);
+      most = max(most, limit[t]);
       const uint16_t* src = a.q + (ok ? (long long)(it.first_query + query) * a.q_token + h * a.q_head : 0);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -125,37 +141,42 @@ __global__ __launch_bounds__(64 * kWaves) void attention_kernel(AttentionArgs a)
         }
     }
 #pragma unroll
-    for (int o = 1; o < 16; o <<= 1) least = min(least, __shfl_xor(least, o)), most = max(most, __shfl_xor(most, o));
+    for (int o = 1; o < 16; o <<= 1) most = max(most, __shfl_xor(most, o));
     const int end = min(it.end, most);
 
     f32x4_t o[MT][DT];
-    float m[MT], l[MT], unit = 7.5e-37f, unit_inv = 1.f / 7.5e-37f;   // (o counts in `unit`: the largest scale of a value so far)
+    float m[MT], l[MT], unit = 7.5e-37f;                      // (o counts in `unit`: the largest scale of a value so far)
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       m[t] = -INFINITY, l[t] = 0.f;
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    for (int key = it.begin + (it.whole ? wave * kKeys : 0); key < end; key += it.whole ? kWaves * kKeys : kKeys) {
-      // the blocks of 16 keys that this lane reads: of keys (for the scores' rows) and of values
-      const int kb = key + 16 * (r >> 2), vb = key + 16 * g;
-      const int kp = kb < it.tokens ? it.table[kb / a.c.page] : -1, vp = vb < it.tokens ? it.table[vb / a.c.page] : -1;
-      const bool k_ok = (unsigned)kp < (unsigned)a.c.n_pages, v_ok = (unsigned)vp < (unsigned)a.c.n_pages;
-      const long long k_row = k_ok ? ((long long)kp * a.c.heads + it.head) * a.c.page + kb % a.c.page : 0;
-      const long long v_row = v_ok ? ((long long)vp * a.c.heads + it.head) * a.c.page + vb % a.c.page : 0;
-      const int8_t* kt = a.c.k + (k_row + (r & 3)) * dim + 16 * g;
-      const int8_t* vt = a.c.v + v_row * dim + r * 16;
-      u32x4_t k[4][NB], v[DT];
+    // The blocks of 16 keys that this lane reads: of keys (for the scores' rows), of values, and of its own key's scales.  Their pages are looked up a step ahead, the keys are
+    // asked for while the scores are turned into probabilities, the values while the scores are made.
+    int page_k, page_v, page_s;
+    const auto page_of = [&](int key) { return it.table[min(key, it.tokens - 1) / a.c.page]; };
+    const auto look_up = [&](int key) { page_k = page_of(key + 16 * (r >> 2)), page_v = page_of(key + 16 * g), page_s = page_of(key + lane / 16 * 16); };
+    u32x4_t k[4][NB], v[DT];
+    const auto request_keys = [&](int key) {
+      const Block16 at(a, it, key + 16 * (r >> 2), page_k);
+      const int8_t* from = a.c.k + (at.row + (r & 3)) * dim + 16 * g;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) k[t][b] = 64 * b + 16 * g < dim ? *(const u32x4_t*)(kt + 4 * t * dim + 64 * b) : u32x4_t{0, 0, 0, 0};
-      f32x4_t ks[4], vs[4];
+        for (int t = 0; t < 4; ++t) k[t][b] = *(const u32x4_t*)(from + 4 * t * dim + (64 * b + 16 * g < dim ? 64 * b : -16 * g));
+    };
+    constexpr int STEP = kWaves * kKeys;
+    int key = it.begin + wave * kKeys;
+    if (key < end) look_up(key), request_keys(key);
+    for (; key < end; key += STEP) {
+      const Block16 at(a, it, key + 16 * g, page_v), as(a, it, key + lane / 16 * 16, page_s);
+      float scale_k = a.c.k_scale[as.row + lane % 16], scale_v = a.c.v_scale[as.row + lane % 16];
+      const int8_t* from = a.c.v + at.row * dim + r * 16;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) ks[t] = *(const f32x4_t*)(a.c.k_scale + v_row + 4 * t), vs[t] = *(const f32x4_t*)(a.c.v_scale + v_row + 4 * t);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) v[d] = 16 * d < dim ? *(const u32x4_t*)(vt + 256 * d) : u32x4_t{0, 0, 0, 0};
-
+      for (int d = 0; d < DT; ++d) v[d] = *(const u32x4_t*)(from + (16 * d < dim ? 256 * d : 0));
+      look_up(key + STEP);
+      __builtin_amdgcn_sched_barrier(0);
       f32x4_t s[MT][4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
@@ -169,59 +190,69 @@ __global__ __launch_bounds__(64 * kWaves) void attention_kernel(AttentionArgs a)
 #pragma unroll
             for (int j = 0; j < MT; ++j) s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, q[j][b][half], s[j][t], 0, 0, 0);
           }
-        ks[t] *= a.scale2;
       }
+      __builtin_amdgcn_sched_barrier(0);
+      request_keys(key + STEP);
+      __builtin_amdgcn_sched_barrier(0);
+      // the scales of the step's keys, one a lane, go round through LDS
+      const float known = as.ok && key + lane < it.tokens && scale_v < INFINITY ? scale_v : 0.f;
       float rescale = 1.f;
-      {
-        float big = 0.f;
-        const int there = v_ok ? it.tokens - vb : 0;
+      if (__any(known > unit)) {
+        float big = known;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) big = fmaxf(big, 4 * t + e < there && vs[t][e] < INFINITY ? vs[t][e] : 0.f);
-        if (__any(big > unit)) {
-          big = fmaxf(big, __shfl_xor(big, 16));
-          big = fmaxf(big, __shfl_xor(big, 32));
-          big = fmaxf(big, unit);
-          rescale = unit / big;
-          unit = big, unit_inv = 1.f / big;
-        }
+        for (int x = 32; x; x >>= 1) big = fmaxf(big, __shfl_xor(big, x));
+        rescale = unit / big;
+        unit = big;
       }
+      s_scale[wave][0][lane] = scale_k * a.scale2;
+      s_scale[wave][1][lane] = scale_v * (1.f / unit);
       f16x8_t p[MT][2];
 #pragma unroll
       for (int j = 0; j < MT; ++j) {
-        const int seen = v_ok ? limit[j] - vb : 0;             // of this lane's 16 keys
-        float top = m[j];
+        const int seen = at.ok ? limit[j] - key - 16 * g : 0;  // of this lane's 16 keys
+        float top = -INFINITY;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t) {
+          const f32x4_t ks = *(const f32x4_t*)&s_scale[wave][0][16 * g + 4 * t];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            s[j][t][e] = 4 * t + e < seen ? s[j][t][e] * ks[t][e] : -INFINITY;
+            s[j][t][e] = 4 * t + e < seen ? s[j][t][e] * ks[e] : -INFINITY;
             top = fmaxf(top, s[j][t][e]);
           }
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float base = top == -INFINITY ? 0.f : top, keep = __builtin_amdgcn_exp2f(m[j] - base);
-        m[j] = top;
+        }
+        float keep = rescale;
+        if (__any(top > m[j] + kSlack)) {
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float to = fmaxf(m[j], top), factor = __builtin_amdgcn_exp2f(m[j] - (to == -INFINITY ? 0.f : to));
+          m[j] = to;
+          l[j] *= factor;
+          keep *= factor;
+        }
+        const float base = m[j] == -INFINITY ? 0.f : m[j];
         float sum = 0.f;
         u32x4_t w[2];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
+          const f32x4_t vs = *(const f32x4_t*)&s_scale[wave][1][16 * g + 4 * t];
           float pv[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float x = __builtin_amdgcn_exp2f(s[j][t][e] - base);
             sum += x;
-            pv[e] = 4 * t + e < seen ? x * (vs[t][e] * unit_inv) : 0.f;   // (a scale that was never written may be anything)
+            pv[e] = 4 * t + e < seen ? x * vs[e] : 0.f;        // (a scale that was never written may be anything)
           }
           w[t >> 1][2 * (t & 1)] = f2h2(pv[0], pv[1]);
           w[t >> 1][2 * (t & 1) + 1] = f2h2(pv[2], pv[3]);
         }
         p[j][0] = __builtin_bit_cast(f16x8_t, w[0]), p[j][1] = __builtin_bit_cast(f16x8_t, w[1]);
-        l[j] = l[j] * keep + sum;
+        l[j] += sum;
+        if (__any(keep != 1.f)) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[j][d] *= keep * rescale;
+          for (int d = 0; d < DT; ++d) o[j][d] *= keep;
+        }
       }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const f16x8_t v0 = half8(v[d][0], v[d][1]), v1 = half8(v[d][2], v[d][3]);
@@ -239,48 +270,46 @@ __global__ __launch_bounds__(64 * kWaves) void attention_kernel(AttentionArgs a)
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[j][d] *= unit;
     }
-    if (it.whole) {                                            // two by two, the upper ones' state into the lower ones'
+    // the states two by two, the upper ones' into the lower ones'
 #pragma unroll
-      for (int half = kWaves / 2; half; half >>= 1) {
-        if (wave >= half && wave < 2 * half) {
-          float (*to)[64] = s_state[wave - half];
+    for (int half = kWaves / 2; half; half >>= 1) {
+      if (wave >= half && wave < 2 * half) {
+        float (*to)[64] = s_state[wave - half];
 #pragma unroll
-          for (int j = 0; j < MT; ++j) {
-            to[j * (4 * DT + 2)][lane] = m[j], to[j * (4 * DT + 2) + 1][lane] = l[j];
+        for (int j = 0; j < MT; ++j) {
+          to[j * (4 * DT + 2)][lane] = m[j], to[j * (4 * DT + 2) + 1][lane] = l[j];
 #pragma unroll
-            for (int d = 0; d < 4 * DT; ++d) to[j * (4 * DT + 2) + 2 + d][lane] = o[j][d >> 2][d & 3];
-          }
+          for (int d = 0; d < 4 * DT; ++d) to[j * (4 * DT + 2) + 2 + d][lane] = o[j][d >> 2][d & 3];
         }
-        __syncthreads();
-        if (wave < half) {
-          float (*from)[64] = s_state[wave];
-#pragma unroll
-          for (int j = 0; j < MT; ++j) {
-            const float om = from[j * (4 * DT + 2)][lane], top = fmaxf(m[j], om), base = top == -INFINITY ? 0.f : top;
-            const float mine = __builtin_amdgcn_exp2f(m[j] - base), other = __builtin_amdgcn_exp2f(om - base);
-            m[j] = top;
-            l[j] = l[j] * mine + from[j * (4 * DT + 2) + 1][lane] * other;
-#pragma unroll
-            for (int d = 0; d < 4 * DT; ++d) o[j][d >> 2][d & 3] = o[j][d >> 2][d & 3] * mine + from[j * (4 * DT + 2) + 2 + d][lane] * other;
-          }
-        }
-        __syncthreads();
       }
+      __syncthreads();
+      if (wave < half) {
+        float (*from)[64] = s_state[wave];
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+          const float om = from[j * (4 * DT + 2)][lane], top = fmaxf(m[j], om), base = top == -INFINITY ? 0.f : top;
+          const float mine = __builtin_amdgcn_exp2f(m[j] - base), other = __builtin_amdgcn_exp2f(om - base);
+          m[j] = top;
+          l[j] = l[j] * mine + from[j * (4 * DT + 2) + 1][lane] * other;
+#pragma unroll
+          for (int d = 0; d < 4 * DT; ++d) o[j][d >> 2][d & 3] = o[j][d >> 2][d & 3] * mine + from[j * (4 * DT + 2) + 2 + d][lane] * other;
+        }
+      }
+      __syncthreads();
     }
-    if (!it.whole || wave == 0) {
+    if (wave == 0) {
       const int slots = a.own.parts + a.prefix.parts;
 #pragma unroll
       for (int j = 0; j < MT; ++j) {
-        const int row = row_first + 16 * j + r, query = row / a.group, h = it.head * a.group + row - query * a.group;
+        const int row = it.row0 + 16 * j + r, query = row / a.group, h = it.head * a.group + row - query * a.group;
         if (row >= it.rows) continue;
         if (slots > 1) {
-          float* to = a.part + (((long long)(it.first_query + query) * a.heads + h) * slots + it.slot) * (dim + 2);
-          if (g == 0) to[dim] = m[j], to[dim + 1] = l[j];
+          const long long at = ((long long)(it.first_query + query) * a.heads + h) * slots + it.slot;
+          if (g == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m[j], l[j]);
+          if (m[j] == -INFINITY && l[j] == 0.f) continue;      // (nothing seen: its sums are not looked at)
 #pragma unroll
           for (int d = 0; d < DT; ++d)
-            if (16 * d < dim)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) to[16 * d + 4 * g + e] = o[j][d][e];
+            if (16 * d < dim) *(f32x4_t*)(a.part + at * dim + 16 * d + 4 * g) = o[j][d];
         } else {
           uint16_t* to = a.out + (long long)(it.first_query + query) * a.out_token + h * a.out_head;
           const float inv = l[j] == 0.f ? 0.f : 1.f / l[j];
@@ -298,49 +327,338 @@ __global__ __launch_bounds__(64 * kWaves) void attention_kernel(AttentionArgs a)
   }
 }
 
-// The pieces of each row put together: a wavefront per row.
+// Many rows: the four wavefronts of a workgroup have 32 rows each and pass over the same keys, which the workgroup turns into bf16 and fp16 once, in LDS, while the steps before
+// them are multiplied.  S^T = K Q^T in blocks of 32 keys x 32 rows, whose row 8 a + 4 h + b is key 16 (a / 2) + 8 h + 4 (a % 2) + b: a lane of half h then holds eight
+// neighbouring keys at a time, an operand of O^T += V^T P^T as it is.  The values carry their scales here (relative to the largest so far, in fp16), once for all rows.
+template <int NB>
+__global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_kernel(AttentionArgs a) {
+  constexpr int DT = 2 * NB, KP = 128 * NB + 16, VP = 2 * kKeys + 16, KB = kKeys * KP, VB = 64 * NB * VP, CH = 4 * NB;   // pitches (odd numbers of 16-byte places), buffers in bytes
+  extern __shared__ __attribute__((aligned(16))) unsigned char s_kv[];
+  float (*s_ks)[kKeys] = (float (*)[kKeys])(s_kv + 2 * (KB + VB));
+  int* s_ok = (int*)(s_ks + 2);
+  _Float16 (*s_vs)[kKeys] = (_Float16 (*)[kKeys])(s_ok + 4);
+  Item it = item_of(a, (int)blockIdx.x, 32 * kWaves);
+  const int step_rows = (it.prefix ? a.prefix : a.own).tiles * 32 * kWaves;
+  for (; it.row0 < it.rows; it.row0 += step_rows) {           // (once, unless a sequence has more queries than was said)
+    int lane = threadIdx.x & 63, dim = a.c.dim;
+    asm volatile("" : "+v"(lane), "+s"(dim));                 // (nothing is made before this loop, and kept in registers through it)
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, half = lane >> 5, thread = 64 * wave + lane;
+    const int row = it.row0 + wave * 32 + r, query = row / a.group, h = it.head * a.group + row - query * a.group;
+    const bool have = row < it.rows;
+    const int limit = !have ? 0 : it.prefix ? it.tokens : it.tokens - it.queries + query + 1;
+    // keys that the workgroup, and the wavefront, look at; up to `least` none is hidden from any row
+    int most = limit, least = have ? limit : 0x7fffffff;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) most = max(most, __shfl_xor(most, o)), least = min(least, __shfl_xor(least, o));
+    int last = it.row0 + 32 * kWaves < it.rows ? it.row0 + 32 * kWaves - 1 : it.rows - 1;
+    const int group_most = it.prefix ? it.tokens : it.tokens - it.queries + last / a.group + 1;
+    const int end = min(it.end, group_most);
+    bf16x8_t q[2 * DT];
+    {
+      const uint16_t* src = a.q + (have ? (long long)(it.first_query + query) * a.q_token + h * a.q_head : 0);
+#pragma unroll
+      for (int s = 0; s < 2 * DT; ++s) {
+        const int d = 16 * s + 8 * half;
+        u32x4_t w = {0, 0, 0, 0};
+        if (have && d < dim) {
+          if (a.vec_q) w = *(const u32x4_t*)(src + d);
+          else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e >> 1] |= (uint32_t)src[d + e] << (16 * (e & 1));
+          }
+        }
+        q[s] = __builtin_bit_cast(bf16x8_t, w);
+      }
+    }
+    f32x16_t o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    float m = -INFINITY, l = 0.f, unit = 7.5e-37f;
+
+    // ---- a step's keys and values on their way: 16 bytes of a key (chunk c of key j), 16 keys of a dimension, the scales of key `lane`
+    const int vr = lane & 15, vg = lane >> 4;
+    int next_page = 0;
+    u32x4_t raw_k[NB], raw_v[NB];
+    float scale_k = 0.f, scale_v = 0.f;
+    int raw_key = 0;
+    bool raw_ok = false;
+    const AnyDiv per_page(a.c.page);
+    const auto look_up = [&](int key) { next_page = it.table[per_page(min(key + 16 * vg, it.tokens - 1))]; };   // of this lane's block of 16 keys
+    const auto request = [&](int key) {
+      const int first = key + 16 * vg;
+      raw_key = key;
+      raw_ok = first < it.tokens && (unsigned)next_page < (unsigned)a.c.n_pages;
+      const long long row = raw_ok ? ((long long)next_page * a.c.heads + it.head) * a.c.page + (first - per_page(first) * a.c.page) : 0;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int id = thread + 256 * i, j = id / CH, c = id - j * CH;
+        const long long at = (long long)(uint32_t)__shfl((int)row, j & 48) | (long long)__shfl((int)(row >> 32), j & 48) << 32;
+        raw_k[i] = *(const u32x4_t*)(a.c.k + (at + j % 16) * dim + (16 * c < dim ? 16 * c : 0));   // (what lies behind dim meets zeros of q)
+      }
+      const int8_t* v = a.c.v + row * dim + vr * 16;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) raw_v[i] = *(const u32x4_t*)(v + (16 * (wave * NB + i) < dim ? 256 * (wave * NB + i) : 0));
+      scale_k = a.c.k_scale[row + vr], scale_v = a.c.v_scale[row + vr];
+    };
+    // they become operands in buffer b; returns what o is to be multiplied by, since it counts in `unit`
+    const auto store = [&](int b) {
+      unsigned char *k = s_kv + b * (KB + VB), *v = k + KB;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int id = thread + 256 * i, j = id / CH, c = id - j * CH;
+        *(bf16x8_t*)(k + j * KP + 32 * c) = whole8(raw_k[i][0], raw_k[i][1]);
+        *(bf16x8_t*)(k + j * KP + 32 * c + 16) = whole8(raw_k[i][2], raw_k[i][3]);
+      }
+      const float known = raw_ok && raw_key + lane < it.tokens && scale_v < INFINITY ? scale_v : 0.f;
+      float rescale = 1.f;
+      if (__any(known > unit)) {                              // (the same for every wavefront)
+        float big = known;
+#pragma unroll
+        for (int x = 32; x; x >>= 1) big = fmaxf(big, __shfl_xor(big, x));
+        rescale = unit / big;
+        unit = big;
+      }
+      s_vs[wave][lane] = (_Float16)(known * (1.f / unit));    // (this wavefront's own: they go round its lanes)
+      f16x8_t by[2];
+#pragma unroll
+      for (int p = 0; p < 2; ++p) by[p] = *(const f16x8_t*)&s_vs[wave][16 * vg + 8 * p];
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) *(f16x8_t*)(v + (16 * (wave * NB + i) + vr) * VP + 32 * vg + 16 * p) = half8(raw_v[i][2 * p], raw_v[i][2 * p + 1]) * by[p];
+      if (wave == 0) {                                        // (a value scale that is no number makes the score one that is none: for the rows that see it)
+        s_ks[b][lane] = scale_v < INFINITY ? scale_k * a.scale2 : __builtin_nanf("");
+        const uint64_t there = __ballot(raw_ok && vr == 0);
+        if (lane == 0) s_ok[b] = (int)((there & 1) | (there >> 15 & 2) | (there >> 30 & 4) | (there >> 45 & 8));
+      }
+      return rescale;
+    };
+
+    float pending = 1.f;                                      // what o is multiplied by before the next step's product
+    __syncthreads();
+    if (it.begin < end) {
+      look_up(it.begin);
+      request(it.begin);
+      pending = store(0);
+      look_up(it.begin + kKeys);
+      request(it.begin + kKeys);
+    }
+    int b = 0;
+    for (int key = it.begin; key < end; key += kKeys, b ^= 1) {
+      __syncthreads();
+      look_up(key + 2 * kKeys);
+      if (key < most) {
+        const unsigned char *k = s_kv + b * (KB + VB), *v = k + KB;
+        f32x16_t s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+          const int j = 32 * t + 16 * (r >> 4) + 8 * (r >> 2 & 1) + 4 * (r >> 3 & 1) + (r & 3);
+#pragma unroll
+          for (int i = 0; i < 2 * DT; ++i) {
+            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t*)(k + j * KP + 32 * i + 16 * half), q[i], s[t], 0, 0, 0);
+            if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (else the operands of all products are read at once, and registers spill)
+          }
+        }
+        // exponents relative to m (to 0 before a first maximum), in place of the scores
+        const int ok = s_ok[b];
+        const bool open = key + kKeys <= least && ok == 15;
+        float base = m == -INFINITY ? 0.f : m, top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const f32x4_t ks = *(const f32x4_t*)&s_ks[b][32 * t + 16 * (x >> 1) + 8 * half + 4 * (x & 1)];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[t][4 * x + e] = __builtin_fmaf(s[t][4 * x + e], ks[e], -base);
+          }
+        if (!open) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int j = 32 * t + 16 * (e >> 3) + 8 * half + 4 * (e >> 2 & 1) + (e & 3);
+              if (!(key + j < limit && (ok >> (2 * t + (e >> 3)) & 1))) s[t][e] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) top = fmx_raw(top, s[t][e]);
+        float keep = pending;
+        pending = 1.f;
+        if (__any(top > (m == -INFINITY ? -INFINITY : kSlack))) {
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float up = m == -INFINITY ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f);
+          const float factor = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-up);
+          if (m != -INFINITY || top != -INFINITY) m = base + up;
+          l *= factor;
+          keep *= factor;
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[t][e] -= up;
+        }
+        if (__any(keep != 1.f)) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[d] *= keep;
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          u32x4_t w[2];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float p0 = __builtin_amdgcn_exp2f(s[t][2 * e]), p1 = __builtin_amdgcn_exp2f(s[t][2 * e + 1]);
+            sum += p0 + p1;
+            w[e >> 2][e & 3] = f2h2(p0, p1);
+          }
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const f16x8_t*)(v + (32 * d + r) * VP + 64 * t + 32 * c + 16 * half), __builtin_bit_cast(f16x8_t, w[c]), o[d], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        l += sum;
+      }
+      if (key + kKeys < end) {
+        const float next = store(b ^ 1);
+        pending *= next;
+        request(key + 2 * kKeys);
+      }
+    }
+    l += __shfl_xor(l, 32);
+    // (o counts in the unit of the last step that was multiplied: `pending` is 1, or there was none after it)
+    const float in = unit * pending;
+    if (have) {
+      const int slots = a.own.parts + a.prefix.parts;
+      if (slots > 1) {
+        const long long at = ((long long)(it.first_query + query) * a.heads + h) * slots + it.slot;
+        if (half == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m, l);
+        if (m != -INFINITY || l != 0.f) {                     // (nothing seen: its sums are not looked at)
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              if (32 * d + 8 * x < dim)
+                *(f32x4_t*)(a.part + at * dim + 32 * d + 8 * x + 4 * half) = f32x4_t{o[d][4 * x] * in, o[d][4 * x + 1] * in, o[d][4 * x + 2] * in, o[d][4 * x + 3] * in};
+        }
+      } else {
+        uint16_t* to = a.out + (long long)(it.first_query + query) * a.out_token + h * a.out_head;
+        const float inv = l == 0.f ? 0.f : in / l;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (32 * d + 8 * x < dim) {
+              const uint32_t lo = f2bf2(o[d][4 * x] * inv, o[d][4 * x + 1] * inv), hi = f2bf2(o[d][4 * x + 2] * inv, o[d][4 * x + 3] * inv);
+              uint16_t* at = to + 32 * d + 8 * x + 4 * half;
+              if (a.vec_out) *(uint2*)at = make_uint2(lo, hi);
+              else at[0] = (uint16_t)lo, at[1] = (uint16_t)(lo >> 16), at[2] = (uint16_t)hi, at[3] = (uint16_t)(hi >> 16);
+            }
+      }
+    }
+  }
+}
+
+// The pieces of a row put together by a workgroup: every wavefront weighs them all, then groups of dim / 4 lanes add four dimensions each of several pieces at a time.
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
-  const int row = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63, slots = a.own.parts + a.prefix.parts, dim = a.c.dim;
-  if (row >= a.n_queries * a.heads) return;
-  const float* from = a.part + (long long)row * slots * (dim + 2);
-  float top = -INFINITY;
-  for (int s = lane; s < slots; s += 64) top = fmaxf(top, from[s * (dim + 2) + dim]);
+  __shared__ float s_w[2 * kMostParts];
+  __shared__ f32x4_t s_o[256];
+  const int row = (int)blockIdx.x, lane = threadIdx.x & 63, slots = a.own.parts + a.prefix.parts, dim = a.c.dim, lanes = dim / 4, groups = 256 / lanes;
+  const float2* ml = (const float2*)a.part_ml + (long long)row * slots;
+  float m[2], l[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int s = lane + 64 * i;
+    const float2 v = s < slots ? ml[s] : make_float2(-INFINITY, 0.f);
+    m[i] = v.x, l[i] = v.y;
+  }
+  float top = fmaxf(m[0], m[1]);
 #pragma unroll
   for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
   const float base = top == -INFINITY ? 0.f : top;
-  float o[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
-  for (int s = 0; s < slots; ++s) {
-    const float* p = from + s * (dim + 2);
-    const float w = __builtin_amdgcn_exp2f(p[dim] - base);
-    l += w * p[dim + 1];
+  float total = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < dim) o[i] += w * p[lane + 64 * i];
+  for (int i = 0; i < 2; ++i) {
+    const bool seen = m[i] != -INFINITY || l[i] != 0.f;       // (l alone: a row that saw what is no number)
+    const float w = seen ? __builtin_amdgcn_exp2f(m[i] - base) : 0.f;
+    if (threadIdx.x < 64 && lane + 64 * i < slots) s_w[lane + 64 * i] = seen && m[i] == -INFINITY ? l[i] : w;
+    total += seen && m[i] == -INFINITY ? l[i] : w * l[i];
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int query = row / a.heads, h = row - query * a.heads;
-  uint16_t* to = a.out + (long long)query * a.out_token + h * a.out_head;
+  total = wave_sum(total);
+  __syncthreads();
+  const int group = (int)threadIdx.x / lanes, d = ((int)threadIdx.x - group * lanes) * 4;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  const float* from = a.part + (long long)row * slots * dim + d;
+  if (group < groups)
+    for (int s0 = group; s0 < slots; s0 += 4 * groups) {
+      float w[4];
+      f32x4_t v[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (lane + 64 * i < dim) to[lane + 64 * i] = f2bf(o[i] * inv);
+      for (int u = 0; u < 4; ++u) {
+        const int s = s0 + u * groups;
+        w[u] = s < slots ? s_w[s] : 0.f;
+        v[u] = w[u] != 0.f ? *(const f32x4_t*)(from + (long long)s * dim) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) o += w[u] * v[u];
+    }
+  s_o[threadIdx.x] = o;
+  __syncthreads();
+  if ((int)threadIdx.x >= lanes) return;
+  for (int g = 1; g < groups; ++g) o += s_o[threadIdx.x + g * lanes];
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  const int query = row / a.heads, h = row - query * a.heads;
+  uint16_t* to = a.out + (long long)query * a.out_token + h * a.out_head + d;
+  const uint32_t lo = f2bf2(o[0] * inv, o[1] * inv), hi = f2bf2(o[2] * inv, o[3] * inv);
+  if (a.vec_out) *(uint2*)to = make_uint2(lo, hi);
+  else to[0] = (uint16_t)lo, to[1] = (uint16_t)(lo >> 16), to[2] = (uint16_t)hi, to[3] = (uint16_t)(hi >> 16);
 }
 
+// One launch over the segments whose kernel is that of row_tiles (attention_split).
 template <int NB>
-int attention(const AttentionArgs& a, hipStream_t st) {
-  const int grid = (a.prefix.parts * a.prefix.tiles + a.n_seqs * a.own.tiles * a.own.parts) * a.c.heads;
-  if (a.row_tiles == 1) attention_kernel<NB, 1><<<grid, 64 * kWaves, 0, st>>>(a);
-  else attention_kernel<NB, 2><<<grid, 64 * kWaves, 0, st>>>(a);
-  if (attention_slots(a) > 1) attention_join_kernel<<<(a.n_queries * a.heads + 3) / 4, 256, 0, st>>>(a);
+int attention_rows(const AttentionArgs& a, int row_tiles, int grid, hipStream_t st) {
+  if (row_tiles == 1) attention_kernel<NB, 1><<<grid, 64 * kWaves, 0, st>>>(a);
+  else if (row_tiles == 2) attention_kernel<NB < 3 ? NB : 2, 2><<<grid, 64 * kWaves, 0, st>>>(a);   // (attention_split)
+  else {
+    static std::atomic<bool> raised{false};
+    const hipError_t e = raise_lds_limit(attention_tile_kernel<NB>, raised);
+    if (e != hipSuccess) return (int)e;
+    constexpr int lds = 2 * (kKeys * (128 * NB + 16) + 64 * NB * (2 * kKeys + 16) + 4 * kKeys) + 16 + kWaves * 2 * kKeys;
+    attention_tile_kernel<NB><<<grid, 64 * kWaves, lds, st>>>(a);
+  }
+  return (int)hipGetLastError();
+}
+template <int NB>
+int attention(AttentionArgs a, hipStream_t st) {
+  const int front = a.prefix.parts * a.prefix.tiles * a.c.heads, own = a.n_seqs * a.own.tiles * a.own.parts * a.c.heads;
+  if (front && a.prefix.row_tiles == a.own.row_tiles) {
+    if (const int e = attention_rows<NB>(a, a.own.row_tiles, front + own, st)) return e;
+  } else {
+    if (front)
+      if (const int e = attention_rows<NB>(a, a.prefix.row_tiles, front, st)) return e;
+    a.skip_prefix = 1;
+    if (const int e = attention_rows<NB>(a, a.own.row_tiles, own, st)) return e;
+  }
+  if (attention_slots(a) > 1) attention_join_kernel<<<a.n_queries * a.heads, 256, 0, st>>>(a);
   return (int)hipGetLastError();
 }
 
-// Pieces of `tokens` keys such that `tiles` row tiles in all make some workgroups per unit, none shorter than two steps of a workgroup.
-void share_out(AttentionShare& s, long long rows, int row_tiles, long long times, long long tokens) {
-  s.whole = rows <= 16 * row_tiles;
-  s.tiles = (int)std::max(1ll, (rows + 16 * row_tiles * (s.whole ? 1 : kWaves) - 1) / (16 * row_tiles * (s.whole ? 1 : kWaves)));
-  const long long want = std::max(1ll, 1024 / std::max(1ll, s.tiles * times)), step = kKeys * (s.whole ? kWaves : 1);
-  const long long most = std::max(1ll, std::min(64ll, tokens / (2 * step)));
-  const long long parts = std::min(want, most);
+// Up to 32 rows: 16 or 32 for every wavefront, which share the keys; more: 32 for each.  The keys are cut in pieces until there are enough workgroups for the units (`want`), none
+// shorter than two steps of every wavefront that takes turns with it.
+// Heads of more than 128 values leave no registers for 32 rows: those go in two tiles of 16.
+void share_out(AttentionShare& s, int dim, long long rows, long long times, long long tokens) {
+  s.row_tiles = rows > 32 ? 0 : rows <= 16 || dim > 128 ? 1 : 2;
+  const long long tile = s.row_tiles ? 16 * s.row_tiles : 32 * kWaves, step = kKeys * (s.row_tiles ? kWaves : 1), want = s.row_tiles ? 2048 : 512;
+  s.tiles = (int)std::max(1ll, (rows + tile - 1) / tile);
+  const long long most = std::max(1ll, std::min<long long>(kMostParts, tokens / (2 * step)));
+  const long long parts = std::min(std::max(1ll, want / std::max(1ll, s.tiles * times)), most);
   s.part_len = (int)(std::max(1ll, (tokens + parts * step - 1) / (parts * step)) * step);
   s.parts = (int)std::max(1ll, (tokens + s.part_len - 1) / s.part_len);
 }
@@ -348,10 +666,8 @@ void share_out(AttentionShare& s, long long rows, int row_tiles, long long times
 }  // namespace
 
 void attention_split(AttentionArgs& a, int max_queries, int max_length) {
-  const long long own = (long long)max_queries * a.group, all = (long long)a.n_queries * a.group;
-  a.row_tiles = own <= 16 && (a.prefix_len == 0 || all <= 16) ? 1 : 2;
-  share_out(a.own, own, a.row_tiles, (long long)std::max(1, a.n_seqs) * a.c.heads, max_length);
-  if (a.prefix_len > 0) share_out(a.prefix, all, a.row_tiles, a.c.heads, a.prefix_len);
+  share_out(a.own, a.c.dim, (long long)max_queries * a.group, (long long)std::max(1, a.n_seqs) * a.c.heads, max_length);
+  if (a.prefix_len > 0) share_out(a.prefix, a.c.dim, (long long)a.n_queries * a.group, a.c.heads, a.prefix_len);
   else a.prefix = AttentionShare{1, 0, kKeys, 1};
 }
 

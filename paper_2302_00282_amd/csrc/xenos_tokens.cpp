@@ -97,7 +97,7 @@ xenos_status attention_of(const xenos_cache* cache, const xenos_attention_args* 
   a.prefix_len = p->prefix_length;
   attention_split(a, std::min(p->max_queries, p->n_queries), (int)std::min<long long>(p->max_length, (long long)p->table_stride * cache->page_tokens));
   const long long own = (long long)a.n_seqs * a.own.tiles * a.own.parts, front = (long long)a.prefix.tiles * a.prefix.parts;
-  if ((own + front) * cache->heads > kMostGroups || (long long)p->n_queries * p->heads > 4 * kMostGroups)
+  if ((own + front) * cache->heads > kMostGroups || (long long)p->n_queries * p->heads > 2 * kMostGroups)
     return fail(XENOS_EUNSUPPORTED, "%s: %d queries of %d sequences are more than one launch holds", who, p->n_queries, p->n_seqs);
   *bytes = attention_slots(a) > 1 ? (size_t)p->n_queries * p->heads * attention_slots(a) * (cache->head_dim + 2) * 4 : 0;
   return XENOS_OK;
@@ -202,6 +202,7 @@ xenos_status xenos_attention(const xenos_cache* cache, const xenos_attention_arg
   a.q = (const uint16_t*)p->d_q, a.out = (uint16_t*)p->d_out;
   a.q_token = p->q_token_stride, a.q_head = p->q_head_stride, a.out_token = p->out_token_stride, a.out_head = p->out_head_stride;
   a.starts = p->d_starts, a.lengths = p->d_lengths, a.tables = p->d_tables, a.prefix_table = p->d_prefix_table, a.part = (float*)d_workspace;
+  a.part_ml = a.part + (size_t)p->n_queries * p->heads * attention_slots(a) * cache->head_dim;
   a.vec_q = aligned(a.q, 16) && a.q_token % 8 == 0 && a.q_head % 8 == 0;
   a.vec_out = aligned(a.out, 8) && a.out_token % 4 == 0 && a.out_head % 4 == 0;
   a.scale2 = p->scale * 1.44269504088896340736f;

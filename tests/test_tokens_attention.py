@@ -16,6 +16,7 @@ class Batch:
 
     def __init__(self, lengths, heads, dim, page, prefix=0, spare=2, seed=1):
         g = torch.Generator().manual_seed(seed)
+        torch.manual_seed(seed)                                 # (for what is drawn on the GPU)
         need = [-(-n // page) for n in lengths]
         front = -(-prefix // page)
         n_pages = front + sum(need) + spare
@@ -65,10 +66,12 @@ class Batch:
                         continue
                     p = torch.softmax(kk @ x * scale, 0)
                     out[starts[b] + i, h] = p @ vv
-                    # a score is off by at most dim + 6 steps of its terms' sizes (log 2 e and the scales among the factors); a probability by that, by its own rounding to bf16
-                    # and by the sum's; the result is rounded once more
+                    # a score is off by at most dim + 6 steps of its terms' sizes (log 2 e and the scales among the factors); a probability by that, by its own rounding
+                    # (with its value's scale, to fp16 in steps of 2^-24 of the largest scale at the least: the probability of the largest score is at least 1 there) and by the sum's;
+                    # the result is rounded once more
                     off = (q.shape[2] + 6) * U32 * (kk.abs() @ x.abs()).max() * scale
-                    bound[starts[b] + i, h] = (U16 + 2.1 * off + (seen / 16 + 40) * U32) * (p @ vv.abs()) + U16 * out[starts[b] + i, h].abs()
+                    least = 2.0 ** -25 * 127 * seen * v[h // group].abs().max() / 100          # (a largest whole number of 100 at least is drawn)
+                    bound[starts[b] + i, h] = (U16 + 2.1 * off + (seen / 16 + 40) * U32) * (p @ vv.abs()) + U16 * out[starts[b] + i, h].abs() + least
         return out, bound * 1.02 + 1e-30
 
 
