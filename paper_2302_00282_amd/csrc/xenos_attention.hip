@@ -17,15 +17,19 @@ namespace {
 constexpr int kKeys = 64;                                     // of a step
 constexpr int kWaves = 4, kMostParts = 64;                    // of a workgroup, of a segment
 
-// Eight bytes as bf16: whole numbers up to 127, exact.
+// Eight bytes as bf16: whole numbers up to 127, exact.  One conversion a byte (the compiler makes two instructions of the cast) and one a pair.
+template <int B>
+__device__ __forceinline__ float byte_of(uint32_t v) {
+  float r;
+  if constexpr (B == 0) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(r) : "v"(v));
+  else if constexpr (B == 1) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(r) : "v"(v));
+  else if constexpr (B == 2) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(r) : "v"(v));
+  else asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(r) : "v"(v));
+  return r;
+}
 __device__ __forceinline__ bf16x8_t whole8(uint32_t lo, uint32_t hi) {
-  u32x4_t w;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const uint32_t v = e < 2 ? lo : hi;
-    w[e] = f2bf2((float)(int8_t)(v >> (16 * (e & 1))), (float)(int8_t)(v >> (16 * (e & 1) + 8)));
-  }
-  return __builtin_bit_cast(bf16x8_t, w);
+  return __builtin_bit_cast(bf16x8_t, (u32x4_t){f2bf2(byte_of<0>(lo), byte_of<1>(lo)), f2bf2(byte_of<2>(lo), byte_of<3>(lo)),
+                                               f2bf2(byte_of<0>(hi), byte_of<1>(hi)), f2bf2(byte_of<2>(hi), byte_of<3>(hi))});
 }
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
@@ -86,6 +90,12 @@ __device__ __forceinline__ Item item_of(const AttentionArgs& a, int at, int tile
   it.begin = part * s.part_len;
   it.end = part == s.parts - 1 || it.begin + s.part_len > it.tokens ? it.tokens : it.begin + s.part_len;
   return it;
+}
+
+__device__ __forceinline__ float max3_raw(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
 }
 
 // Where a block of 16 keys of a segment lies: its first row among the cache's, if it has a page.
@@ -205,7 +215,7 @@ __global__ __launch_bounds__(64 * kWaves, MT == 1 && NB <= 2 ? 4 - NB : 1) void 
         unit = big;
       }
       s_scale[wave][0][lane] = scale_k * a.scale2;
-      s_scale[wave][1][lane] = scale_v * (1.f / unit);
+      s_scale[wave][1][lane] = scale_v * __builtin_amdgcn_rcpf(unit);
       f16x8_t p[MT][2];
 #pragma unroll
       for (int j = 0; j < MT; ++j) {
@@ -350,6 +360,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
     int most = limit, least = have ? limit : 0x7fffffff;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) most = max(most, __shfl_xor(most, o)), least = min(least, __shfl_xor(least, o));
+    most = __builtin_amdgcn_readfirstlane(most), least = __builtin_amdgcn_readfirstlane(least);
     int last = it.row0 + 32 * kWaves < it.rows ? it.row0 + 32 * kWaves - 1 : it.rows - 1;
     const int group_most = it.prefix ? it.tokens : it.tokens - it.queries + last / a.group + 1;
     const int end = min(it.end, group_most);
@@ -420,7 +431,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
         rescale = unit / big;
         unit = big;
       }
-      s_vs[wave][lane] = (_Float16)(known * (1.f / unit));    // (this wavefront's own: they go round its lanes)
+      s_vs[wave][lane] = (_Float16)(known * __builtin_amdgcn_rcpf(unit));    // (this wavefront's own: they go round its lanes)
       f16x8_t by[2];
 #pragma unroll
       for (int p = 0; p < 2; ++p) by[p] = *(const f16x8_t*)&s_vs[wave][16 * vg + 8 * p];
@@ -465,7 +476,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
         }
         // exponents relative to m (to 0 before a first maximum), in place of the scores
         const int ok = s_ok[b];
-        const bool open = key + kKeys <= least && ok == 15;
+        const bool open = key + kKeys <= least && __builtin_amdgcn_readfirstlane(ok) == 15;
         float base = m == -INFINITY ? 0.f : m, top = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -476,6 +487,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
             for (int e = 0; e < 4; ++e) s[t][4 * x + e] = __builtin_fmaf(s[t][4 * x + e], ks[e], -base);
           }
         if (!open) {
+          asm volatile("");                                   // (a branch: as selections of every element this is a tenth of a step)
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -487,7 +499,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) top = fmx_raw(top, s[t][e]);
+          for (int e = 0; e < 16; e += 2) top = max3_raw(top, s[t][e], s[t][e + 1]);
         float keep = pending;
         pending = 1.f;
         if (__any(top > (m == -INFINITY ? -INFINITY : kSlack))) {
