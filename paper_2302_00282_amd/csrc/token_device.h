@@ -23,6 +23,13 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// The bare instruction, as fmx_raw
+__device__ __forceinline__ float max3_raw(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 // The step of a row whose largest magnitude has the bits m: q = rint(v inv), and q times scale() stands for v.
 struct RowStep {
   float amp, inv;

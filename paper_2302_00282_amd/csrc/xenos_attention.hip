@@ -92,12 +92,6 @@ __device__ __forceinline__ Item item_of(const AttentionArgs& a, int at, int tile
   return it;
 }
 
-__device__ __forceinline__ float max3_raw(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
-
 // Where a block of 16 keys of a segment lies: its first row among the cache's, if it has a page.
 struct Block16 {
   long long row;

@@ -1,6 +1,6 @@
 // What is read from logits: log probabilities of given tokens, entropy, the likeliest tokens.
 //
-// One pass over a row.  Each lane keeps a running maximum m with s = sum e^(x - m) and t = sum (x - m) e^(x - m), so that log p = x - m - log s and
+// One pass over a row.  Each lane keeps a reference m near the row's maximum with s = sum e^(x - m) and t = sum (x - m) e^(x - m), so that log p = x - m - log s and
 // the entropy is log s - t / s; each wavefront keeps the best tokens it has seen sorted over its lanes, and an element is looked at closely only if it beats the
 // last of those that count.  Order is that of one whole number per element: the value's bits, ordered, above the inverted index.
 #include <algorithm>
@@ -11,11 +11,12 @@ namespace xenos {
 namespace {
 
 constexpr float kLowest = -3.402823466e38f, kLog2e = 1.44269504088896340736f;
+constexpr float kSlack = 8.f;                                 // a maximum is followed when it has grown by more: terms up to e^8 are as exact
 constexpr int kPer = 16, kBlock = 64 * kPer;                  // elements per lane and wavefront at a time
 
 // (bits of v in their order, ties to the lower index); NaN above all, -0 as 0
 __device__ __forceinline__ uint64_t order_of(float v, int index) {
-  const uint32_t u = v != v ? 0x7fc00000u : __float_as_uint(v + 0.f);
+  const uint32_t bits = __float_as_uint(v), u = (bits & 0x7fffffffu) > 0x7f800000u ? 0x7fc00000u : bits == 0x80000000u ? 0u : bits;
   return (uint64_t)(u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) << 32 | (uint32_t)~index;
 }
 __device__ __forceinline__ float value_of(uint64_t o) {
@@ -31,7 +32,9 @@ __device__ __forceinline__ float times_or_zero(float a, float b) {
   return r;
 }
 
-// Maximum and sums of some of a row's elements.  m is finite or +infinity: where nothing was added, s is 0.
+// Sums over some of a row's elements: s = sum e^(x - m), t = sum (x - m) e^(x - m).  The reference m is the maximum, or less by kSlack at most, finite or +infinity; where
+// nothing was added, s is 0.  (x - m is made before it is scaled for the power of 2: x log2 e - m log2 e in one instruction overflows where a mask of the type's lowest
+// value leaves nothing else.)
 struct Sums {
   float m, s, t;
   __device__ __forceinline__ void raise(float to) {           // to >= m
@@ -40,7 +43,7 @@ struct Sums {
     s *= e;
     m = to;
   }
-  __device__ __forceinline__ void add(float x) {              // x <= m, or NaN
+  __device__ __forceinline__ void add(float x) {              // x <= m + kSlack, or NaN
     const float d = x - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
     s += e;
     t += times_or_zero(d, e);                                 // (-infinity adds nothing)
@@ -52,6 +55,8 @@ struct Sums {
     s += o.s;
     t += o.t;
   }
+  __device__ __forceinline__ float logprob(float x) const { return x - m - logf(s); }
+  __device__ __forceinline__ float entropy() const { return logf(s) - t / s; }
 };
 __device__ __forceinline__ uint64_t from_lane(uint64_t v, int lane) {
   return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
@@ -60,25 +65,55 @@ __device__ __forceinline__ uint64_t from_lane(uint64_t v, int lane) {
 // Finishes a row whose sums and best tokens are known.
 template <typename T>
 __device__ __forceinline__ void finish(const LogprobsArgs& a, int row, const Sums& z) {
-  const float ls = logf(z.s);
-  if (a.entropy) a.entropy[row] = ls - z.t / z.s;
+  if (a.entropy) a.entropy[row] = z.entropy();
   if (a.logprob) {
     const long long t = a.targets[row];
-    a.logprob[row] = t >= 0 && t < a.vocab ? Tr<T>::ld(a.x, row * a.stride + t) - z.m - ls : 0.f;
+    a.logprob[row] = t >= 0 && t < a.vocab ? z.logprob(Tr<T>::ld(a.x, row * a.stride + t)) : 0.f;
   }
 }
 
-// Elements that beat the last one that counts (`last`, 0 while there are fewer than `top`) join the sorted list `best`, one at a time.
-__device__ __forceinline__ void best_insert(uint64_t& best, uint64_t& last, uint64_t o, int top, int lane) {
-  for (uint64_t found; (found = __ballot(o > last)) != 0;) {
-    const int from = __builtin_ctzll(found);
-    const uint64_t take = from_lane(o, from);
-    const int at = __builtin_popcountll(__ballot(best > take));
-    const uint64_t up = (uint64_t)(uint32_t)__shfl_up((int)(best >> 32), 1) << 32 | (uint32_t)__shfl_up((int)best, 1);
-    best = lane < at ? best : lane == at ? take : up;
-    last = from_lane(best, top - 1);
-    if (lane == from) o = 0;
+// v of the lane before (lane 0: anything)
+__device__ __forceinline__ uint32_t lane_before(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x138, 0xf, 0xf, false); }   // (wave_shr:1)
+
+// v with `value` in one lane, both the same for all lanes
+__device__ __forceinline__ uint32_t set_lane(uint32_t v, uint32_t value, int lane) {
+  asm("s_mov_b32 m0, %2\n v_writelane_b32 %0, %1, m0" : "+v"(v) : "s"(__builtin_amdgcn_readfirstlane(value)), "s"(__builtin_amdgcn_readfirstlane(lane)) : "m0");
+  return v;
+}
+
+// The best elements a wavefront has seen, by order_of: lane i has the i-th; `last`, the top-th, is 0 while there are fewer.
+struct Best {
+  uint32_t lo = 0, hi = 0;
+  uint64_t last = 0;
+  __device__ __forceinline__ void insert(uint64_t o, int top) {   // o > last, the same for all lanes
+    const bool before = all() > o;
+    const int at = __builtin_popcountll(__ballot(before));
+    const uint32_t up_lo = lane_before(lo), up_hi = lane_before(hi);
+    lo = before ? lo : up_lo, hi = before ? hi : up_hi;
+    lo = set_lane(lo, (uint32_t)o, at), hi = set_lane(hi, (uint32_t)(o >> 32), at);     // (at < top: it beats the last one)
+    last = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, top - 1) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)lo, top - 1);
   }
+  // an element of each lane, 0 for none
+  __device__ __forceinline__ void offer(uint64_t o, int top) {
+    for (uint64_t found = __ballot(o > last); found; found &= found - 1) {
+      const uint64_t take = from_lane(o, __builtin_ctzll(found));
+      if (take > last) insert(take, top);
+    }
+  }
+  __device__ __forceinline__ uint64_t all() const { return (uint64_t)hi << 32 | lo; }
+};
+
+// The rank-th largest (from 0) of the lanes' values, by a sorting network: halves of 2, 4 .. 64 lanes in turn, each merged in steps.
+__device__ __forceinline__ float lane_rank(float v, int rank, int lane) {
+#pragma unroll
+  for (int size = 2; size <= 64; size <<= 1)
+#pragma unroll
+    for (int step = size >> 1; step; step >>= 1) {
+      const float o = __shfl_xor(v, step);
+      const bool down = (lane & size) == 0, first = (lane & step) == 0;
+      v = down == first ? fmx_raw(v, o) : fminf(v, o);
+    }
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), rank));
 }
 
 // The four wavefronts' sums and lists put together, and the row's results, or the part's, written.
@@ -114,7 +149,7 @@ __device__ __forceinline__ void join_waves(const LogprobsArgs& a, Sums z, uint64
     if (partial) to[3 + 2 * at] = (uint32_t)mine, to[4 + 2 * at] = (uint32_t)(mine >> 32);
     else {
       a.top_token[(long long)row * a.top + at] = index_of(mine);
-      a.top_logprob[(long long)row * a.top + at] = value_of(mine) - z.m - logf(z.s);
+      a.top_logprob[(long long)row * a.top + at] = z.logprob(value_of(mine));
     }
   }
   // (a part that has fewer elements than are asked for: the places behind them)
@@ -128,15 +163,15 @@ __device__ __forceinline__ void join_waves(const LogprobsArgs& a, Sums z, uint64
 
 // A workgroup per part of a row; its wavefronts take blocks of the part in turn.
 template <typename T, bool TOP>
-__global__ __launch_bounds__(256) void logprobs_kernel(LogprobsArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = (int)blockIdx.x / a.parts, part = (int)blockIdx.x - row * a.parts;
+__global__ __launch_bounds__(256, 8) void logprobs_kernel(LogprobsArgs a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = (int)blockIdx.x / a.parts, part = (int)blockIdx.x - row * a.parts;
   const T* x = (const T*)a.x + row * a.stride;
   const int begin = part * a.part_len, end = begin + a.part_len < a.vocab ? begin + a.part_len : a.vocab;
   // vectors start where memory is aligned to 16 bytes, before `begin` by up to CE - 1 elements
   constexpr int CE = Tr<T>::CE, NV = kPer / CE;
   const int shift = (int)(((uintptr_t)(x + begin) & 15) / sizeof(T)), first = begin - shift + lane * CE;
   Sums z{kLowest, 0.f, 0.f};
-  uint64_t best = 0, last = 0;                                // lane i: the i-th best so far; the last one that counts
+  Best best;
   for (int b = wave * kBlock; b < end - begin + shift; b += 4 * kBlock) {
     float f[kPer];
 #pragma unroll
@@ -150,23 +185,41 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobsArgs a) {
     }
     float top = f[0];
 #pragma unroll
-    for (int e = 1; e < kPer; ++e) top = fmaxf(top, f[e]);
-    z.raise(fmaxf(z.m, top));
+    for (int e = 1; e + 1 < kPer; e += 2) top = max3_raw(top, f[e], f[e + 1]);
+    top = fmx_raw(top, f[kPer - 1]);
+    if (__any(top > z.m + kSlack)) z.raise(fmaxf(z.m, top));
 #pragma unroll
     for (int e = 0; e < kPer; ++e) z.add(f[e]);
-    // (what equals the last one comes after it: its index is higher than any seen in an earlier block)
-    if (TOP && (last == 0 || __any(top > value_of(last) || z.s != z.s))) {
+    if (!TOP) continue;
+    const int i0 = begin - shift + b;                         // (of lane 0)
+    if (__any(z.s != z.s)) {                                  // (NaN, now or before: every element in full)
 #pragma unroll
       for (int c = 0; c < NV; ++c)
 #pragma unroll
         for (int e = 0; e < CE; ++e) {
-          const int i = first + b + c * 64 * CE + e;
-          const uint64_t o = i >= begin && i < end ? order_of(f[c * CE + e], i) : 0;
-          best_insert(best, last, o, a.top, lane);
+          const int i = i0 + (c * 64 + lane) * CE + e;
+          best.offer(i >= begin && i < end ? order_of(f[c * CE + e], i) : 0, a.top);
         }
+      continue;
     }
+    // What equals the last one comes after it, since its index is higher than any seen in an earlier block.  The first block has no last one: the top-th of the lanes' largest
+    // elements is one that as many elements reach.  The few elements that pass are looked at by the scalar unit.
+    const bool from_here = best.last == 0;
+    const float over = from_here ? lane_rank(top, a.top - 1, lane) : value_of(best.last);
+    if (!from_here && !__any(top > over)) continue;
+#pragma unroll
+    for (int c = 0; c < NV; ++c)
+#pragma unroll
+      for (int e = 0; e < CE; ++e) {
+        const float v = f[c * CE + e];
+        for (uint64_t found = from_here ? __ballot(v >= over) : __ballot(v > over); found; found &= found - 1) {
+          const int from = __builtin_ctzll(found), i = i0 + (c * 64 + from) * CE + e;
+          const uint64_t take = order_of(__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), from)), i);
+          if (i >= begin && i < end && take > best.last) best.insert(take, a.top);
+        }
+      }
   }
-  join_waves<T, TOP>(a, z, best, row, part, a.parts > 1);
+  join_waves<T, TOP>(a, z, best.all(), row, part, a.parts > 1);
 }
 
 // The parts of a row put together, in the order of the parts.
@@ -179,13 +232,13 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobsArgs a) {
     const uint32_t* p = parts + lane * words;
     z.m = __uint_as_float(p[0]), z.s = __uint_as_float(p[1]), z.t = __uint_as_float(p[2]);
   }
-  uint64_t best = 0, last = 0;
+  Best best;
   if (TOP)
     for (int i = wave; i < a.parts; i += 4) {
       const uint32_t* p = parts + i * words + 3 + 2 * lane;
-      best_insert(best, last, lane < a.top ? (uint64_t)p[1] << 32 | p[0] : 0, a.top, lane);
+      best.offer(lane < a.top ? (uint64_t)p[1] << 32 | p[0] : 0, a.top);
     }
-  join_waves<T, TOP>(a, z, best, row, 0, false);
+  join_waves<T, TOP>(a, z, best.all(), row, 0, false);
 }
 
 template <typename T>
