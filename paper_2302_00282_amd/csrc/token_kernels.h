@@ -51,6 +51,7 @@ struct CacheWriteArgs {
   long long k_token, k_head, v_token, v_head;
   const long long* slots;
   int tokens;
+  int vec;                                                   // fours of elements are aligned as such
 };
 struct CacheReadArgs {
   CacheArgs c;

@@ -157,8 +157,9 @@ xenos_status xenos_cache_write(const xenos_cache* cache, int n_tokens, const voi
   if (!d_k || !d_v || !d_slots) return fail(XENOS_EINVAL, "xenos_cache_write: NULL argument");
   if (!aligned(d_k, size_of(dtype)) || !aligned(d_v, size_of(dtype)) || !aligned(d_slots, 8)) return fail(XENOS_EINVAL, "xenos_cache_write: a buffer is not aligned");
   if (k_token_stride < 0 || k_head_stride < 0 || v_token_stride < 0 || v_head_stride < 0) return fail(XENOS_ESHAPE, "xenos_cache_write: negative stride");
-  if ((long long)n_tokens * cache->heads > 4 * kMostGroups) return fail(XENOS_EUNSUPPORTED, "xenos_cache_write: %d tokens of %d heads are more than one launch holds", n_tokens, cache->heads);
+  if ((n_tokens + 127ll) / 128 * 8 * cache->heads > 2 * kMostGroups || n_tokens > (1 << 30)) return fail(XENOS_EUNSUPPORTED, "xenos_cache_write: %d tokens of %d heads are more than one launch holds", n_tokens, cache->heads);
   a.k = d_k, a.v = d_v, a.k_token = k_token_stride, a.k_head = k_head_stride, a.v_token = v_token_stride, a.v_head = v_head_stride, a.slots = d_slots, a.tokens = n_tokens;
+  a.vec = aligned(d_k, 4 * size_of(dtype)) && aligned(d_v, 4 * size_of(dtype)) && (k_token_stride | k_head_stride | v_token_stride | v_head_stride) % 4 == 0;
   return launched(launch_cache_write(a, dtype, hip_stream), "xenos_cache_write");
 }
 
@@ -170,7 +171,7 @@ xenos_status xenos_cache_read(const xenos_cache* cache, int n_tokens, const long
   if (n_tokens == 0) return XENOS_OK;
   if (!d_k || !d_v || !d_slots) return fail(XENOS_EINVAL, "xenos_cache_read: NULL argument");
   if (!aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_slots, 8)) return fail(XENOS_EINVAL, "xenos_cache_read: a buffer is not aligned (k and v: to 16 bytes)");
-  if ((long long)n_tokens * cache->heads > 4 * kMostGroups) return fail(XENOS_EUNSUPPORTED, "xenos_cache_read: %d tokens of %d heads are more than one launch holds", n_tokens, cache->heads);
+  if ((n_tokens + 127ll) / 128 * 8 * cache->heads > 2 * kMostGroups || n_tokens > (1 << 30)) return fail(XENOS_EUNSUPPORTED, "xenos_cache_read: %d tokens of %d heads are more than one launch holds", n_tokens, cache->heads);
   a.slots = d_slots, a.k = d_k, a.v = d_v, a.tokens = n_tokens;
   return launched(launch_cache_read(a, dtype, hip_stream), "xenos_cache_read");
 }
