@@ -23,7 +23,7 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// The bare instruction, as fmx_raw
+// The bare instruction, as fmx_raw: for values from loads and plain arithmetic (the compiler adds no waits for what an instruction in assembly reads)
 __device__ __forceinline__ float max3_raw(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));

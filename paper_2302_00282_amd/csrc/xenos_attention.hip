@@ -493,7 +493,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int e = 0; e < 16; e += 2) top = max3_raw(top, s[t][e], s[t][e + 1]);
+          for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[t][e]), s[t][e + 1]);
         float keep = pending;
         pending = 1.f;
         if (__any(top > (m == -INFINITY ? -INFINITY : kSlack))) {

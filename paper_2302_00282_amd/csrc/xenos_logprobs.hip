@@ -25,13 +25,6 @@ __device__ __forceinline__ float value_of(uint64_t o) {
 }
 __device__ __forceinline__ int index_of(uint64_t o) { return (int)~(uint32_t)o; }
 
-// a b, and 0 where either is 0
-__device__ __forceinline__ float times_or_zero(float a, float b) {
-  float r;
-  asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-  return r;
-}
-
 // Sums over some of a row's elements: s = sum e^(x - m), t = sum (x - m) e^(x - m).  The reference m is the maximum, or less by kSlack at most, finite or +infinity; where
 // nothing was added, s is 0.  (x - m is made before it is scaled for the power of 2: x log2 e - m log2 e in one instruction overflows where a mask of the type's lowest
 // value leaves nothing else.)
@@ -46,7 +39,7 @@ struct Sums {
   __device__ __forceinline__ void add(float x) {              // x <= m + kSlack, or NaN
     const float d = x - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
     s += e;
-    t += times_or_zero(d, e);                                 // (-infinity adds nothing)
+    t = __builtin_fmaf(fmaxf(d, kLowest), e, t);              // (-infinity adds nothing: 0 times a number; a NaN is in s)
   }
   __device__ __forceinline__ void join(Sums o) {
     const float to = fmaxf(m, o.m);
@@ -75,22 +68,17 @@ __device__ __forceinline__ void finish(const LogprobsArgs& a, int row, const Sum
 // v of the lane before (lane 0: anything)
 __device__ __forceinline__ uint32_t lane_before(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x138, 0xf, 0xf, false); }   // (wave_shr:1)
 
-// v with `value` in one lane, both the same for all lanes
-__device__ __forceinline__ uint32_t set_lane(uint32_t v, uint32_t value, int lane) {
-  asm("s_mov_b32 m0, %2\n v_writelane_b32 %0, %1, m0" : "+v"(v) : "s"(__builtin_amdgcn_readfirstlane(value)), "s"(__builtin_amdgcn_readfirstlane(lane)) : "m0");
-  return v;
-}
-
 // The best elements a wavefront has seen, by order_of: lane i has the i-th; `last`, the top-th, is 0 while there are fewer.
 struct Best {
   uint32_t lo = 0, hi = 0;
   uint64_t last = 0;
   __device__ __forceinline__ void insert(uint64_t o, int top) {   // o > last, the same for all lanes
+    const int lane = threadIdx.x & 63;
     const bool before = all() > o;
     const int at = __builtin_popcountll(__ballot(before));
     const uint32_t up_lo = lane_before(lo), up_hi = lane_before(hi);
     lo = before ? lo : up_lo, hi = before ? hi : up_hi;
-    lo = set_lane(lo, (uint32_t)o, at), hi = set_lane(hi, (uint32_t)(o >> 32), at);     // (at < top: it beats the last one)
+    lo = lane == at ? (uint32_t)o : lo, hi = lane == at ? (uint32_t)(o >> 32) : hi;
     last = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, top - 1) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)lo, top - 1);
   }
   // an element of each lane, 0 for none
@@ -109,7 +97,7 @@ __device__ __forceinline__ float lane_rank(float v, int rank, int lane) {
   for (int size = 2; size <= 64; size <<= 1)
 #pragma unroll
     for (int step = size >> 1; step; step >>= 1) {
-      const float o = __shfl_xor(v, step);
+      const float o = __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute((lane ^ step) << 2, (int)__float_as_uint(v)));
       const bool down = (lane & size) == 0, first = (lane & step) == 0;
       v = down == first ? fmx_raw(v, o) : fminf(v, o);
     }
@@ -192,30 +180,36 @@ __global__ __launch_bounds__(256, 8) void logprobs_kernel(LogprobsArgs a) {
     for (int e = 0; e < kPer; ++e) z.add(f[e]);
     if (!TOP) continue;
     const int i0 = begin - shift + b;                         // (of lane 0)
-    if (__any(z.s != z.s)) {                                  // (NaN, now or before: every element in full)
+    // What equals the last one comes after it, since its index is higher than any seen in an earlier block.  The first block has no last one: the top-th of the lanes' largest
+    // elements is one that as many elements reach.  There, where many may be equal, and where there is a NaN, now or before, elements are compared in full by every lane; else
+    // the few that pass are looked at by the scalar unit.
+    const bool from_here = best.last == 0, nan = __any(z.s != z.s);
+    if (from_here || nan) {
+      int here = lane;
+      asm volatile("" : "+v"(here));                          // (what this rare path needs is made in it, not held through the others)
+      const float over = nan ? -INFINITY : lane_rank(top, a.top - 1, here);
+      const int mine = i0 + here * CE;
 #pragma unroll
       for (int c = 0; c < NV; ++c)
 #pragma unroll
         for (int e = 0; e < CE; ++e) {
-          const int i = i0 + (c * 64 + lane) * CE + e;
-          best.offer(i >= begin && i < end ? order_of(f[c * CE + e], i) : 0, a.top);
+          const int i = mine + c * 64 * CE + e;
+          const float v = f[c * CE + e];
+          best.offer(i >= begin && i < end && !(v < over) ? order_of(v, i) : 0, a.top);
         }
       continue;
     }
-    // What equals the last one comes after it, since its index is higher than any seen in an earlier block.  The first block has no last one: the top-th of the lanes' largest
-    // elements is one that as many elements reach.  The few elements that pass are looked at by the scalar unit.
-    const bool from_here = best.last == 0;
-    const float over = from_here ? lane_rank(top, a.top - 1, lane) : value_of(best.last);
-    if (!from_here && !__any(top > over)) continue;
+    const float over = value_of(best.last);
+    if (!__any(top > over)) continue;
 #pragma unroll
     for (int c = 0; c < NV; ++c)
 #pragma unroll
       for (int e = 0; e < CE; ++e) {
         const float v = f[c * CE + e];
-        for (uint64_t found = from_here ? __ballot(v >= over) : __ballot(v > over); found; found &= found - 1) {
+        for (uint64_t found = __ballot(v > over); found; found &= found - 1) {   // (what lies outside the row is -infinity: not more than anything)
           const int from = __builtin_ctzll(found), i = i0 + (c * 64 + from) * CE + e;
           const uint64_t take = order_of(__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), from)), i);
-          if (i >= begin && i < end && take > best.last) best.insert(take, a.top);
+          if (take > best.last) best.insert(take, a.top);
         }
       }
   }
