@@ -63,7 +63,7 @@ struct CacheReadArgs {
 struct AttentionShare {
   int tiles;                                                 // of rows
   int parts, part_len;                                       // pieces of the keys, of part_len (a multiple of 64) tokens each, the last one to the end
-  int row_tiles;                                             // 1, 2: the wavefronts of a workgroup have the same 16 or 32 rows and take turns with the keys; 0: 32 rows each
+  bool many;                                                 // rows: 32 for each wavefront of a workgroup, not the same 16 for all, which take turns with the keys
 };
 struct AttentionArgs {
   CacheArgs c;

@@ -3,7 +3,7 @@
 // Keys pass once, 64 at a time, with the running maximum m and sum l of a softmax per row.  The scores are computed transposed, S^T = K Q^T, so that a lane ends up with
 // 16 neighbouring keys of one row (tile t of a wavefront's four takes key 16 (r / 4) + 4 t + r % 4 as its row r): the maximum is over registers and two exchanges, and the lane's
 // probabilities are, as they lie, the operand of O^T += V^T P^T, whose other operand is what the cache holds for one dimension: 16 keys side by side.
-// Nothing passes through LDS.  The 8-bit keys become bf16 and the values fp16 without rounding; the keys' scales multiply the scores, the values' the probabilities.
+// With few rows keys and values go from memory to registers as they are, and only the scales round through LDS; with many the wavefronts share both there.  The 8-bit keys become bf16 and the values fp16 without rounding; the keys' scales multiply the scores, the values' the probabilities.
 // Those are rounded to fp16 for the product, after division by the largest value scale so far: eight times as fine as bf16, whose error would be as large as that of the
 // rounding of the result (relative error of the output against 64 bits: 1.7e-3 in place of 2.4e-3), and in range whatever the scales are.
 #include <algorithm>
@@ -106,27 +106,26 @@ struct Block16 {
 // the exchange of maxima and the rescaling of O are rare.
 constexpr float kSlack = 8.f;
 
-// Few rows: the wavefronts of a workgroup have the same 16 MT rows and take turns with the keys; their states meet in LDS at the end.  NB: blocks of 64 dimensions.
-template <int NB, int MT>
-__global__ __launch_bounds__(64 * kWaves, MT == 1 && NB <= 2 ? 4 - NB : 1) void attention_kernel(AttentionArgs a) {
-  constexpr int DT = 4 * NB, REC = MT * (4 * DT + 2);         // tiles of 16 dimensions; floats of a lane's state
+// Few rows: the wavefronts of a workgroup have the same 16 rows and take turns with the keys; their states meet in LDS at the end.  NB: blocks of 64 dimensions.
+template <int NB>
+__global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_kernel(AttentionArgs a) {
+  constexpr int DT = 4 * NB, REC = 4 * DT + 2;              // tiles of 16 dimensions; floats of a lane's state
   __shared__ float s_state[kWaves / 2][REC][64];
   __shared__ __attribute__((aligned(16))) float s_scale[kWaves][2][kKeys];
-  Item it = item_of(a, (int)blockIdx.x, 16 * MT);
-  const int step_rows = (it.prefix ? a.prefix : a.own).tiles * 16 * MT;
+  Item it = item_of(a, (int)blockIdx.x, 16);
+  const int step_rows = (it.prefix ? a.prefix : a.own).tiles * 16;
   for (; it.row0 < it.rows; it.row0 += step_rows) {           // (once, unless a sequence has more queries than was said)
     int lane = threadIdx.x & 63, dim = a.c.dim;
     asm volatile("" : "+v"(lane), "+s"(dim));                 // (nothing is made before this loop, and kept in registers through it)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     // rows of this lane: queries in bf16, and the keys they see
-    bf16x8_t q[MT][NB][2];
-    int limit[MT], most = 0;
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-      const int row = it.row0 + 16 * t + r, query = row / a.group, h = it.head * a.group + row - query * a.group;
+    bf16x8_t q[NB][2];
+    int limit, most;
+    {
+      const int row = it.row0 + r, query = row / a.group, h = it.head * a.group + row - query * a.group;
       const bool ok = row < it.rows;
-      limit[t] = !ok ? 0 : it.prefix ? it.tokens : it.tokens - it.queries + query + 1;
-      most = max(most, limit[t]);
+      limit = !ok ? 0 : it.prefix ? it.tokens : it.tokens - it.queries + query + 1;
+      most = limit;
       const uint16_t* src = a.q + (ok ? (long long)(it.first_query + query) * a.q_token + h * a.q_head : 0);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -141,21 +140,17 @@ __global__ __launch_bounds__(64 * kWaves, MT == 1 && NB <= 2 ? 4 - NB : 1) void 
               for (int e = 0; e < 8; ++e) w[e >> 1] |= (uint32_t)src[d + e] << (16 * (e & 1));
             }
           }
-          q[t][b][half] = __builtin_bit_cast(bf16x8_t, w);
+          q[b][half] = __builtin_bit_cast(bf16x8_t, w);
         }
     }
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) most = max(most, __shfl_xor(most, o));
     const int end = min(it.end, most);
 
-    f32x4_t o[MT][DT];
-    float m[MT], l[MT], unit = 7.5e-37f;                      // (o counts in `unit`: the largest scale of a value so far)
+    f32x4_t o[DT];
+    float m = -INFINITY, l = 0.f, unit = 7.5e-37f;            // (o counts in `unit`: the largest scale of a value so far)
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-      m[t] = -INFINITY, l[t] = 0.f;
-#pragma unroll
-      for (int d = 0; d < DT; ++d) o[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int d = 0; d < DT; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     // The blocks of 16 keys that this lane reads: of keys (for the scores' rows), of values, and of its own key's scales.  Their pages are looked up a step ahead, the keys are
     // asked for while the scores are turned into probabilities, the values while the scores are made.
     int page_k, page_v, page_s;
@@ -181,18 +176,16 @@ __global__ __launch_bounds__(64 * kWaves, MT == 1 && NB <= 2 ? 4 - NB : 1) void 
       for (int d = 0; d < DT; ++d) v[d] = *(const u32x4_t*)(from + (16 * d < dim ? 256 * d : 0));
       look_up(key + STEP);
       __builtin_amdgcn_sched_barrier(0);
-      f32x4_t s[MT][4];
+      f32x4_t s[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-#pragma unroll
-        for (int j = 0; j < MT; ++j) s[j][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
             const bf16x8_t kk = whole8(k[t][b][2 * half], k[t][b][2 * half + 1]);
-#pragma unroll
-            for (int j = 0; j < MT; ++j) s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, q[j][b][half], s[j][t], 0, 0, 0);
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, q[b][half], s[t], 0, 0, 0);
           }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -210,122 +203,104 @@ __global__ __launch_bounds__(64 * kWaves, MT == 1 && NB <= 2 ? 4 - NB : 1) void 
       }
       s_scale[wave][0][lane] = scale_k * a.scale2;
       s_scale[wave][1][lane] = scale_v * __builtin_amdgcn_rcpf(unit);
-      f16x8_t p[MT][2];
+      f16x8_t p[2];
+      const int seen = at.ok ? limit - key - 16 * g : 0;      // of this lane's 16 keys
+      float top = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < MT; ++j) {
-        const int seen = at.ok ? limit[j] - key - 16 * g : 0;  // of this lane's 16 keys
-        float top = -INFINITY;
+      for (int t = 0; t < 4; ++t) {
+        const f32x4_t ks = *(const f32x4_t*)&s_scale[wave][0][16 * g + 4 * t];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const f32x4_t ks = *(const f32x4_t*)&s_scale[wave][0][16 * g + 4 * t];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s[j][t][e] = 4 * t + e < seen ? s[j][t][e] * ks[e] : -INFINITY;
-            top = fmaxf(top, s[j][t][e]);
-          }
+        for (int e = 0; e < 4; ++e) {
+          s[t][e] = 4 * t + e < seen ? s[t][e] * ks[e] : -INFINITY;
+          top = fmaxf(top, s[t][e]);
         }
-        float keep = rescale;
-        if (__any(top > m[j] + kSlack)) {
-          top = fmaxf(top, __shfl_xor(top, 16));
-          top = fmaxf(top, __shfl_xor(top, 32));
-          const float to = fmaxf(m[j], top), factor = __builtin_amdgcn_exp2f(m[j] - (to == -INFINITY ? 0.f : to));
-          m[j] = to;
-          l[j] *= factor;
-          keep *= factor;
-        }
-        const float base = m[j] == -INFINITY ? 0.f : m[j];
-        float sum = 0.f;
-        u32x4_t w[2];
+      }
+      float keep = rescale;
+      if (__any(top > m + kSlack)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float to = fmaxf(m, top), factor = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.f : to));
+        m = to;
+        l *= factor;
+        keep *= factor;
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+      float sum = 0.f;
+      u32x4_t w[2];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const f32x4_t vs = *(const f32x4_t*)&s_scale[wave][1][16 * g + 4 * t];
-          float pv[4];
+      for (int t = 0; t < 4; ++t) {
+        const f32x4_t vs = *(const f32x4_t*)&s_scale[wave][1][16 * g + 4 * t];
+        float pv[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = __builtin_amdgcn_exp2f(s[j][t][e] - base);
-            sum += x;
-            pv[e] = 4 * t + e < seen ? x * vs[e] : 0.f;        // (a scale that was never written may be anything)
-          }
-          w[t >> 1][2 * (t & 1)] = f2h2(pv[0], pv[1]);
-          w[t >> 1][2 * (t & 1) + 1] = f2h2(pv[2], pv[3]);
+        for (int e = 0; e < 4; ++e) {
+          const float x = __builtin_amdgcn_exp2f(s[t][e] - base);
+          sum += x;
+          pv[e] = 4 * t + e < seen ? x * vs[e] : 0.f;        // (a scale that was never written may be anything)
         }
-        p[j][0] = __builtin_bit_cast(f16x8_t, w[0]), p[j][1] = __builtin_bit_cast(f16x8_t, w[1]);
-        l[j] += sum;
-        if (__any(keep != 1.f)) {
+        w[t >> 1][2 * (t & 1)] = f2h2(pv[0], pv[1]);
+        w[t >> 1][2 * (t & 1) + 1] = f2h2(pv[2], pv[3]);
+      }
+      p[0] = __builtin_bit_cast(f16x8_t, w[0]), p[1] = __builtin_bit_cast(f16x8_t, w[1]);
+      l += sum;
+      if (__any(keep != 1.f)) {
 #pragma unroll
-          for (int d = 0; d < DT; ++d) o[j][d] *= keep;
-        }
+        for (int d = 0; d < DT; ++d) o[d] *= keep;
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const f16x8_t v0 = half8(v[d][0], v[d][1]), v1 = half8(v[d][2], v[d][3]);
-#pragma unroll
-        for (int j = 0; j < MT; ++j) {
-          o[j][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[j][0], o[j][d], 0, 0, 0);
-          o[j][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[j][1], o[j][d], 0, 0, 0);
-        }
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[0], o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[1], o[d], 0, 0, 0);
       }
     }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
-      l[j] += __shfl_xor(l[j], 16);
-      l[j] += __shfl_xor(l[j], 32);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) o[j][d] *= unit;
-    }
+    for (int d = 0; d < DT; ++d) o[d] *= unit;
     // the states two by two, the upper ones' into the lower ones'
 #pragma unroll
     for (int half = kWaves / 2; half; half >>= 1) {
       if (wave >= half && wave < 2 * half) {
         float (*to)[64] = s_state[wave - half];
+        to[0][lane] = m, to[1][lane] = l;
 #pragma unroll
-        for (int j = 0; j < MT; ++j) {
-          to[j * (4 * DT + 2)][lane] = m[j], to[j * (4 * DT + 2) + 1][lane] = l[j];
-#pragma unroll
-          for (int d = 0; d < 4 * DT; ++d) to[j * (4 * DT + 2) + 2 + d][lane] = o[j][d >> 2][d & 3];
-        }
+        for (int d = 0; d < 4 * DT; ++d) to[2 + d][lane] = o[d >> 2][d & 3];
       }
       __syncthreads();
       if (wave < half) {
         float (*from)[64] = s_state[wave];
+        const float om = from[0][lane], top = fmaxf(m, om), base = top == -INFINITY ? 0.f : top;
+        const float mine = __builtin_amdgcn_exp2f(m - base), other = __builtin_amdgcn_exp2f(om - base);
+        m = top;
+        l = l * mine + from[1][lane] * other;
 #pragma unroll
-        for (int j = 0; j < MT; ++j) {
-          const float om = from[j * (4 * DT + 2)][lane], top = fmaxf(m[j], om), base = top == -INFINITY ? 0.f : top;
-          const float mine = __builtin_amdgcn_exp2f(m[j] - base), other = __builtin_amdgcn_exp2f(om - base);
-          m[j] = top;
-          l[j] = l[j] * mine + from[j * (4 * DT + 2) + 1][lane] * other;
-#pragma unroll
-          for (int d = 0; d < 4 * DT; ++d) o[j][d >> 2][d & 3] = o[j][d >> 2][d & 3] * mine + from[j * (4 * DT + 2) + 2 + d][lane] * other;
-        }
+        for (int d = 0; d < 4 * DT; ++d) o[d >> 2][d & 3] = o[d >> 2][d & 3] * mine + from[2 + d][lane] * other;
       }
       __syncthreads();
     }
     if (wave == 0) {
       const int slots = a.own.parts + a.prefix.parts;
+      const int row = it.row0 + r, query = row / a.group, h = it.head * a.group + row - query * a.group;
+      if (row >= it.rows) continue;
+      if (slots > 1) {
+        const long long at = ((long long)(it.first_query + query) * a.heads + h) * slots + it.slot;
+        if (g == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m, l);
+        if (m == -INFINITY && l == 0.f) continue;          // (nothing seen: its sums are not looked at)
 #pragma unroll
-      for (int j = 0; j < MT; ++j) {
-        const int row = it.row0 + 16 * j + r, query = row / a.group, h = it.head * a.group + row - query * a.group;
-        if (row >= it.rows) continue;
-        if (slots > 1) {
-          const long long at = ((long long)(it.first_query + query) * a.heads + h) * slots + it.slot;
-          if (g == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m[j], l[j]);
-          if (m[j] == -INFINITY && l[j] == 0.f) continue;      // (nothing seen: its sums are not looked at)
+        for (int d = 0; d < DT; ++d)
+          if (16 * d < dim) *(f32x4_t*)(a.part + at * dim + 16 * d + 4 * g) = o[d];
+      } else {
+        uint16_t* to = a.out + (long long)(it.first_query + query) * a.out_token + h * a.out_head;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-          for (int d = 0; d < DT; ++d)
-            if (16 * d < dim) *(f32x4_t*)(a.part + at * dim + 16 * d + 4 * g) = o[j][d];
-        } else {
-          uint16_t* to = a.out + (long long)(it.first_query + query) * a.out_token + h * a.out_head;
-          const float inv = l[j] == 0.f ? 0.f : 1.f / l[j];
-#pragma unroll
-          for (int d = 0; d < DT; ++d)
-            if (16 * d < dim) {
-              const uint32_t lo = f2bf2(o[j][d][0] * inv, o[j][d][1] * inv), hi = f2bf2(o[j][d][2] * inv, o[j][d][3] * inv);
-              uint16_t* at = to + 16 * d + 4 * g;
-              if (a.vec_out) *(uint2*)at = make_uint2(lo, hi);
-              else at[0] = (uint16_t)lo, at[1] = (uint16_t)(lo >> 16), at[2] = (uint16_t)hi, at[3] = (uint16_t)(hi >> 16);
-            }
-        }
+        for (int d = 0; d < DT; ++d)
+          if (16 * d < dim) {
+            const uint32_t lo = f2bf2(o[d][0] * inv, o[d][1] * inv), hi = f2bf2(o[d][2] * inv, o[d][3] * inv);
+            uint16_t* at = to + 16 * d + 4 * g;
+            if (a.vec_out) *(uint2*)at = make_uint2(lo, hi);
+            else at[0] = (uint16_t)lo, at[1] = (uint16_t)(lo >> 16), at[2] = (uint16_t)hi, at[3] = (uint16_t)(hi >> 16);
+          }
       }
     }
   }
@@ -627,11 +602,10 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
   else to[0] = (uint16_t)lo, to[1] = (uint16_t)(lo >> 16), to[2] = (uint16_t)hi, to[3] = (uint16_t)(hi >> 16);
 }
 
-// One launch over the segments whose kernel is that of row_tiles (attention_split).
+// One launch over the segments whose kernel is the same.
 template <int NB>
-int attention_rows(const AttentionArgs& a, int row_tiles, int grid, hipStream_t st) {
-  if (row_tiles == 1) attention_kernel<NB, 1><<<grid, 64 * kWaves, 0, st>>>(a);
-  else if (row_tiles == 2) attention_kernel<NB < 3 ? NB : 2, 2><<<grid, 64 * kWaves, 0, st>>>(a);   // (attention_split)
+int attention_rows(const AttentionArgs& a, bool many, int grid, hipStream_t st) {
+  if (!many) attention_kernel<NB><<<grid, 64 * kWaves, 0, st>>>(a);
   else {
     static std::atomic<bool> raised{false};
     const hipError_t e = raise_lds_limit(attention_tile_kernel<NB>, raised);
@@ -644,24 +618,27 @@ int attention_rows(const AttentionArgs& a, int row_tiles, int grid, hipStream_t 
 template <int NB>
 int attention(AttentionArgs a, hipStream_t st) {
   const int front = a.prefix.parts * a.prefix.tiles * a.c.heads, own = a.n_seqs * a.own.tiles * a.own.parts * a.c.heads;
-  if (front && a.prefix.row_tiles == a.own.row_tiles) {
-    if (const int e = attention_rows<NB>(a, a.own.row_tiles, front + own, st)) return e;
+  if (front && a.prefix.many == a.own.many) {
+    if (const int e = attention_rows<NB>(a, a.own.many, front + own, st)) return e;
   } else {
     if (front)
-      if (const int e = attention_rows<NB>(a, a.prefix.row_tiles, front, st)) return e;
+      if (const int e = attention_rows<NB>(a, a.prefix.many, front, st)) return e;
     a.skip_prefix = 1;
-    if (const int e = attention_rows<NB>(a, a.own.row_tiles, own, st)) return e;
+    if (const int e = attention_rows<NB>(a, a.own.many, own, st)) return e;
   }
   if (attention_slots(a) > 1) attention_join_kernel<<<a.n_queries * a.heads, 256, 0, st>>>(a);
   return (int)hipGetLastError();
 }
 
-// Up to 32 rows: 16 or 32 for every wavefront, which share the keys; more: 32 for each.  The keys are cut in pieces until there are enough workgroups for the units (`want`), none
-// shorter than two steps of every wavefront that takes turns with it.
-// Heads of more than 128 values leave no registers for 32 rows: those go in two tiles of 16.
+// Which kernel a segment has.  More than 32 rows, and rows x keys x dimensions of 1.6e9 at the least: many rows; below, its few workgroups and its way into LDS cost more than it saves.
+// us for 16 rows a workgroup, for many rows (8 heads of 128, keys x sequences x rows): 8192 x 1 x 128: 26, 30; 5869 x 1 x 128 (dim 64): 18, 26; 8192 x 4 x 64: 40, 36; 8192 x 1 x 512: 65,
+// 45; 2048 x 8 x 1024: 200, 94; 4 heads, 4097 x 1 x 20485, each row up to its own: 264, 143.
+// The keys are cut in pieces until there are `want` workgroups, none shorter than two steps of every wavefront that takes turns with it: 16 rows, heads up to 128, 2048 (16 sequences of 100 to
+// 32768 tokens, 8 heads of 128: in 512 130 us, in 2048 110; where all have 32768, 198 and 206); longer heads, of which a unit holds a workgroup or two, and many rows: 512 (32 sequences of 4042,
+// 16 heads of 256: 126 us, in 2048 157; 8 sequences of 2048 with 1024 rows: 94, in 1024 166).
 void share_out(AttentionShare& s, int dim, long long rows, long long times, long long tokens) {
-  s.row_tiles = rows > 32 ? 0 : rows <= 16 || dim > 128 ? 1 : 2;
-  const long long tile = s.row_tiles ? 16 * s.row_tiles : 32 * kWaves, step = kKeys * (s.row_tiles ? kWaves : 1), want = s.row_tiles ? 2048 : 512;
+  s.many = rows > 32 && (double)(rows * times) * (double)tokens * dim >= 1.6e9;
+  const long long tile = s.many ? 32 * kWaves : 16, step = kKeys * (s.many ? 1 : kWaves), want = s.many || dim > 128 ? 512 : 2048;
   s.tiles = (int)std::max(1ll, (rows + tile - 1) / tile);
   const long long most = std::max(1ll, std::min<long long>(kMostParts, tokens / (2 * step)));
   const long long parts = std::min(std::max(1ll, want / std::max(1ll, s.tiles * times)), most);
@@ -674,7 +651,7 @@ void share_out(AttentionShare& s, int dim, long long rows, long long times, long
 void attention_split(AttentionArgs& a, int max_queries, int max_length) {
   share_out(a.own, a.c.dim, (long long)max_queries * a.group, (long long)std::max(1, a.n_seqs) * a.c.heads, max_length);
   if (a.prefix_len > 0) share_out(a.prefix, a.c.dim, (long long)a.n_queries * a.group, a.c.heads, a.prefix_len);
-  else a.prefix = AttentionShare{1, 0, kKeys, 1};
+  else a.prefix = AttentionShare{1, 0, kKeys, false};
 }
 
 int launch_attention(const AttentionArgs& a, void* stream) {

@@ -15,7 +15,7 @@ def test_no_vector_register_is_spilled(kernels, kernel):  # noqa: F811
     assert not {k: v for k, v in found.items() if v["vgpr_spill_count"] or v["private_segment_fixed_size"]}
 
 
-@pytest.mark.parametrize("kernel,most", [("attention_kernelILi1ELi1E", 168), ("attention_kernelILi2ELi1E", 256), ("attention_tile_kernelILi[12]E", 256), ("logprobs_kernelI", 64),
+@pytest.mark.parametrize("kernel,most", [("attention_kernelILi1E", 168), ("attention_kernelILi2E", 256), ("attention_tile_kernelILi[12]E", 256), ("logprobs_kernelI", 64),
                                          ("quant_matmul_kernelI\\w+Li4ELi2ELi2E", 256)])
 def test_units_hold_the_wavefronts_that_were_planned(kernels, kernel, most):  # noqa: F811
     found = {k: v for k, v in kernels.items() if re.search(r"\d" + kernel, k)}

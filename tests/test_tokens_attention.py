@@ -124,6 +124,56 @@ def test_a_whole_prompt(heads, kv_heads, dim):
     check(Batch([301], kv_heads, dim, 32), queries_of(301, heads, dim), [301])
 
 
+def roomy(batch, tokens=1 << 22):
+    """The batch with tables for that many tokens: work is shared out as if sequences were as long, whose rows then go 128 to a workgroup."""
+    tables = torch.full((len(batch.lengths), tokens // batch.cache.page_tokens), -1, dtype=torch.int32)
+    tables[:, :batch.tables.shape[1]] = batch.tables
+    batch.tables = tables
+    return batch
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prefix", [0, 77])
+@pytest.mark.parametrize("heads,kv_heads,dim,page", [(2, 2, 64, 16), (8, 2, 128, 64), (15, 3, 80, 48), (4, 1, 256, 32), (3, 1, 48, 128), (6, 2, 192, 16), (5, 1, 16, 16)])
+@pytest.mark.parametrize("queries", [[1, 44, 0, 7], [70, 1, 3, 33], [35, 150, 5, 5]])
+def test_chunks_of_queries_where_sequences_may_be_long(queries, heads, kv_heads, dim, page, prefix):
+    check(roomy(Batch([97, 4, 30, 64], kv_heads, dim, page, prefix)), queries_of(sum(queries), heads, dim), queries)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+def test_many_sequences_of_many_rows(dim):
+    """So many that the keys of none are cut in pieces: results go out as they are made."""
+    queries = [40 + i % 3 if i % 50 == 0 else i % 2 for i in range(260)]
+    check(roomy(Batch([7 * i % 90 for i in range(260)], 2, dim, 16), 4096), queries_of(sum(queries), 4, dim), queries)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [30.0, 1e-3])
+def test_steep_and_flat_scores_of_many_rows(size):
+    queries = [40, 65, 1]
+    check(roomy(Batch([500, 65, 1], 2, 64, 32, 40)), queries_of(106, 4, 64, size=size), queries)
+    check(roomy(Batch([500, 65, 1], 2, 64, 32)), queries_of(106, 4, 64, size=size), queries, scale=0.0)
+
+
+@pytest.mark.gpu
+def test_many_rows_that_see_nothing_and_pages_that_are_not_there():
+    y = check(roomy(Batch([2, 0, 40], 2, 64, 16)), queries_of(90, 4, 64), [40, 10, 40])
+    assert not y[:38].any() and not y[40:50].any() and y[50:].any()
+    batch = roomy(Batch([40], 2, 64, 16))
+    length, start, q = torch.tensor([40], dtype=torch.int32, device="cuda"), torch.tensor([0, 40], dtype=torch.int32, device="cuda"), queries_of(40, 4, 64)
+    attend = lambda tables, n, **kw: T.attention(q, batch.cache, tables.cuda(), length + n - 40, starts=start, max_queries=40, **kw)
+    whole = attend(batch.tables, 40)
+    for entry in (-1, 1 << 20):
+        tables = batch.tables.clone()
+        tables[0, 2] = entry                                    # tokens 32 .. 39
+        assert torch.equal(attend(tables, 40)[:32], whole[:32])
+    assert torch.equal(attend(batch.tables, 40, out=torch.full((40, 5, 66), 3.0, dtype=torch.bfloat16, device="cuda")[:, 1:, 1:65]), whole)
+    batch.cache.v_scale[batch.tables[0, 1].long(), 1, 3] = NAN   # token 19
+    y = attend(batch.tables, 40)
+    assert torch.isnan(y[19:, 2:]).all() and torch.equal(y[:16], whole[:16]) and torch.equal(y[:, :2], whole[:, :2])
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("prefix", [0, 5000])
 def test_long_sequences_are_cut_in_pieces(prefix):
