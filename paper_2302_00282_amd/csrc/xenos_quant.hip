@@ -64,7 +64,7 @@ __device__ __forceinline__ float row_scale(const QuantRowsArgs& a, const RowStep
 
 // One workgroup per row: q = rint(x g 127 / a), a = max|x g|, scale = a / 127 [/ rms(x)].  The norm's factor is one number per row: it
 // cancels in q, so that the rounded values do not depend on how the squares are summed.  A thread keeps its NV x 8 values in registers, one pass over memory
-// (8192 x 8192 bf16: 63 us in two passes, 45 so); NV = 0: rows of any length in two passes, the second from the cache (where there are few of them, the same time: 32 x 25088 takes 7 us).
+// (8192 x 8192 bf16: 63 us in two passes, 45 so: 4.5 TB/s read and written, what memory gives); NV = 0: rows of any length in two passes, the second from the cache (where there are few of them, the same time: 32 x 25088 takes 7 us).
 template <typename T, int NV>
 __global__ __launch_bounds__(1024) void quant_rows_kernel(QuantRowsArgs a) {
   __shared__ uint32_t s_max[16];
@@ -243,7 +243,8 @@ __device__ __forceinline__ void quant_into_lds(const QuantRowsArgs& a, int8_t* q
 
 // Few rows: the weights are the work.  A workgroup has 16 output channels and all of K, which its wavefronts share; every fragment of the weights goes
 // from memory to registers, a lane's 16 bytes of one weight row at a time, and the sums (whole numbers: exact in any order) meet in LDS.
-// OWN: x comes as it is, and every workgroup quantises all of it for itself.
+// Bound by the weights' bytes where there are many (1 x 25088 x 4096: 17.7 us, 5.8 TB/s), by its chain of trips to memory and LDS where there are few.
+// OWN: x comes as it is, and every workgroup quantises all of it for itself (1 x 512 x 2048 in one launch: 5.8 us; linear_in_one).
 template <typename T, int MT, bool OWN>
 __global__ __launch_bounds__(512) void quant_matvec_kernel(QuantMatmulArgs a, QuantRowsArgs qa) {
   __shared__ i32x4_t part[8][MT][64];
@@ -318,6 +319,7 @@ __device__ __forceinline__ void wait_behind(int behind) {
 // K passes in steps of 128 bytes through STAGES stages of LDS that the loads write themselves (whole lines of the cache: with steps of 64 bytes a unit got 16 bytes a cycle).
 // A step is read in two halves, each while the half before it is multiplied; behind the second read the stage is free, and one barrier tells that to all and that the
 // next stage has arrived.
+// Bound by the matrix units: 8192 x 8192 x 8192 takes 510 to 560 us, 2.0 to 2.15 POP/s, with tiles of 256.  Tiles of 64 in shares of K stream weights: 32 x 25088 x 4096 21 us, 4.9 TB/s.
 template <typename T, int WM, int WN, int TM, int TN, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void quant_matmul_kernel(QuantMatmulArgs a, int tiles_m, int tiles_n, int splits) {
   constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN, WAVES = WM * WN, STAGE = (BM + BN) * 128, LOADS = (BM + BN) / 8 / WAVES;
@@ -433,7 +435,7 @@ __global__ __launch_bounds__(64 * WM * WN) void quant_matmul_kernel(QuantMatmulA
   }
 }
 
-// The shares of a product whose K was split, added (whole numbers: in any order), and its results.
+// The shares of a product whose K was split, added (whole numbers: in any order), and its results.  (A thread has eight columns; 32 x 4096 of 8 shares: 4.6 us, a launch and two trips to memory.)
 template <typename T>
 __global__ __launch_bounds__(256) void quant_finish_kernel(QuantMatmulArgs a, int splits) {
   const int eights = a.part_pitch / 8, at = (int)blockIdx.x * 256 + (int)threadIdx.x, m = at / eights, n = (at - m * eights) * 8;
@@ -466,6 +468,7 @@ static int quant_tiles_of(const QuantMatmulArgs& a, int splits, hipStream_t st) 
   return (int)hipGetLastError();
 }
 static long long quant_tiles_in(int M, int N, int edge) { return (long long)((M + edge - 1) / edge) * ((N + edge - 1) / edge); }
+// The largest tiles that leave every unit one.  us in tiles of 256, 128, 64: 8192 x 8192 x 8192: 480 to 590, 563 to 600; 2048 x 4096 x 4096: 57, 42; 512 x 4096 x 4096: -, 25, 16.5.
 template <typename T>
 static int quant_tiles(const QuantMatmulArgs& a, hipStream_t st) {
   if (quant_tiles_in(a.M, a.N, 256) >= 256) return quant_tiles_of<T, 2, 4, 4, 2, 2>(a, 1, st);
