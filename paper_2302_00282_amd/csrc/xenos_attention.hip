@@ -51,7 +51,8 @@ __device__ __forceinline__ uint32_t f2h2(float lo, float hi) { return __builtin_
 struct Item {
   int head;                                                   // of the cache
   const int* table;
-  int tokens;                                                 // of the segment
+  int tokens;                                                 // of the segment that its table holds
+  int length;                                                 // of a sequence: its last query sees the tokens up to this one
   int first_query, queries;
   int row0, rows;                                             // first row of the tile; rows of the item in all (queries times the group)
   int begin, end;                                             // keys
@@ -73,12 +74,12 @@ __device__ __forceinline__ Item item_of(const AttentionArgs& a, int at, int tile
   at /= s.tiles;
   const int part = at % s.parts, seq = at / s.parts;
   if (it.prefix) {
-    it.table = a.prefix_table, it.tokens = a.prefix_len, it.first_query = 0, it.queries = a.n_queries, it.slot = part;
+    it.table = a.prefix_table, it.tokens = it.length = a.prefix_len, it.first_query = 0, it.queries = a.n_queries, it.slot = part;
   } else {
     const long long held = (long long)a.table_stride * a.c.page;
-    const int n = a.lengths[seq];
+    const int n = max(a.lengths[seq], 0);
     it.table = a.tables + (long long)seq * a.table_stride;
-    it.tokens = n < 0 ? 0 : n < held ? n : (int)held;
+    it.length = n, it.tokens = n < held ? n : (int)held;
     const int lo = a.starts ? a.starts[seq] : seq, hi = a.starts ? a.starts[seq + 1] : seq + 1;
     it.first_query = lo < 0 ? 0 : lo < a.n_queries ? lo : a.n_queries;
     it.queries = hi <= it.first_query ? 0 : (hi < a.n_queries ? hi : a.n_queries) - it.first_query;
@@ -91,6 +92,9 @@ __device__ __forceinline__ Item item_of(const AttentionArgs& a, int at, int tile
   it.end = part == s.parts - 1 || it.begin + s.part_len > it.tokens ? it.tokens : it.begin + s.part_len;
   return it;
 }
+
+// The keys of a segment that a query sees, from its first one on.
+__device__ __forceinline__ int seen_by(const Item& it, int query) { return it.prefix ? it.tokens : min(it.tokens, it.length - it.queries + query + 1); }
 
 // Where a block of 16 keys of a segment lies: its first row among the cache's, if it has a page.
 struct Block16 {
@@ -125,7 +129,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_k
     {
       const int row = it.row0 + r, query = row / a.group, h = it.head * a.group + row - query * a.group;
       const bool ok = row < it.rows;
-      limit = !ok ? 0 : it.prefix ? it.tokens : it.tokens - it.queries + query + 1;
+      limit = ok ? seen_by(it, query) : 0;
       most = limit;
       const uint16_t* src = a.q + (ok ? (long long)(it.first_query + query) * a.q_token + h * a.q_head : 0);
 #pragma unroll
@@ -328,15 +332,14 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, half = lane >> 5, thread = 64 * wave + lane;
     const int row = it.row0 + wave * 32 + r, query = row / a.group, h = it.head * a.group + row - query * a.group;
     const bool have = row < it.rows;
-    const int limit = !have ? 0 : it.prefix ? it.tokens : it.tokens - it.queries + query + 1;
+    const int limit = have ? seen_by(it, query) : 0;
     // keys that the workgroup, and the wavefront, look at; up to `least` none is hidden from any row
     int most = limit, least = have ? limit : 0x7fffffff;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) most = max(most, __shfl_xor(most, o)), least = min(least, __shfl_xor(least, o));
     most = __builtin_amdgcn_readfirstlane(most), least = __builtin_amdgcn_readfirstlane(least);
     int last = it.row0 + 32 * kWaves < it.rows ? it.row0 + 32 * kWaves - 1 : it.rows - 1;
-    const int group_most = it.prefix ? it.tokens : it.tokens - it.queries + last / a.group + 1;
-    const int end = min(it.end, group_most);
+    const int end = min(it.end, seen_by(it, last / a.group));
     bf16x8_t q[2 * DT];
     {
       const uint16_t* src = a.q + (have ? (long long)(it.first_query + query) * a.q_token + h * a.q_head : 0);

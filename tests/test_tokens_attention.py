@@ -361,3 +361,77 @@ def test_attention_entries_refuse_before_any_launch():
     with pytest.raises(X.XenosError):
         X.xenos_attention(X.Cache(4, 24, 2, 64, p, p, p, p), X.AttentionArgs(**good), p, 1 << 40)
     X.xenos_attention(cache, X.AttentionArgs(**dict(good, n_queries=0, n_seqs=0, d_q=None)))
+
+
+def defined(q, cache, tables, lengths, starts, scale, prefix_table=None, prefix=0):
+    """(out, what its error may be) in 64 bits for the rows of `starts`, from the formula and the layout alone: a query sees the prefix and, of the tokens that its
+    sequence's table holds in pages of the cache, those up to lengths - queries + its number.
+
+    The error: of a score, dim + 6 steps of its terms' sizes; of a weight (probability times value scale) that, one rounding to fp16 and one to fp32; sums of `seen` terms in 16 lanes
+    at a time; a weight below fp16's normal numbers half of 2^-24 of the row's reference, which its largest weight exceeds by 2^7; one rounding to bf16 at the end."""
+    held = [x.cpu() for x in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+    page, group, dim = cache.page_tokens, q.shape[1] // cache.heads, cache.head_dim
+
+    def keys(table, n):
+        j = torch.arange(min(max(n, 0), len(table) * page))
+        pages = table.long()[j // page]
+        j, pages = j[(pages >= 0) & (pages < cache.n_pages)], pages[(pages >= 0) & (pages < cache.n_pages)]
+        at = j % page
+        return (j, *(x.double().transpose(0, 1) for x in (held[0][pages, :, at], held[1][pages, :, at // 16, :, at % 16], held[2][pages, :, at], held[3][pages, :, at])))
+
+    q = q.double().cpu()
+    out, bound = torch.zeros_like(q), torch.zeros_like(q)
+    rows = [(-1, -(1 << 40), 0, range(len(q)))] + [(b, n, starts[b + 1] - starts[b], range(starts[b], starts[b + 1])) for b, n in enumerate(lengths)]
+    front = keys(torch.zeros(0) if prefix_table is None else prefix_table.cpu(), prefix)
+    for b, n, m, which in rows:                                 # (first as if no row had a sequence)
+        own = keys(torch.zeros(0) if b < 0 else tables[b].cpu(), n)
+        at = torch.cat([front[0] - (1 << 40), own[0]])
+        k, v, ks, vs = (torch.cat(x, 1) for x in zip(front[1:], own[1:]))
+        for i, t in enumerate(which):
+            see = at < n - m + i + 1 if b >= 0 else at < 0
+            for h in range(q.shape[1]):
+                e, c = q[t, h], h // group
+                kk, vv, w = k[c, see] * ks[c, see, None], v[c, see] * vs[c, see, None], vs[c, see]
+                if not len(kk):
+                    out[t, h], bound[t, h] = 0, 0
+                    continue
+                p = torch.softmax(kk @ e * scale, 0)
+                off = (dim + 6) * U32 * (kk.abs() @ e.abs()).max() * abs(scale)
+                size = p @ vv.abs()
+                least = 2.0 ** -32 * 127 * len(p) * (p * w.clamp_min(2.0 ** -88)).max()
+                inner = (2.0 ** -11 + 2.1 * off + (len(p) / 16 + 40) * U32) * size + least
+                out[t, h] = p @ vv
+                bound[t, h] = inner + U16 * (out[t, h].abs() + inner)
+    return out, bound * 1.01 + 1e-38
+
+
+def whole(numbers):
+    return torch.tensor(numbers, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("over", [1, 15, 100, 1000])
+@pytest.mark.parametrize("heads,kv_heads,dim,queries", [(4, 2, 64, 6), (3, 1, 80, 40), (2, 2, 256, 17)])
+def test_queries_of_a_length_beyond_the_table(heads, kv_heads, dim, queries, over):
+    """Which tokens a query sees is counted from the length, not from what the table holds of it."""
+    batch = Batch([64], kv_heads, dim, 16)
+    tables, q, scale = batch.tables[:, :4], queries_of(queries, heads, dim), dim ** -0.5
+    y = T.attention(q, batch.cache, tables.cuda(), whole([64 + over]), starts=whole([0, queries]), max_queries=queries)
+    want, bound = defined(q, batch.cache, tables, [64 + over], [0, queries], scale)
+    assert torch.all((y.double().cpu() - want).abs() <= bound)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("over", [1, 100, 1000])
+@pytest.mark.parametrize("dim", [128, 256])
+def test_many_queries_of_a_length_beyond_the_table(dim, over):
+    queries, held, page = 300, 16384, 16                        # (600 rows on 2 heads: each workgroup has 128 of them)
+    batch = Batch([450], 2, dim, page)
+    tables = torch.full((1, held // page), -1, dtype=torch.int32)
+    tables[0, -28:], tables[0, 5] = batch.tables[0, :28], batch.tables[0, 28]     # (the last 448 tokens, and a page that is there far ahead of them)
+    batch.cache.k_scale[batch.tables[0, 28].long()] = 0.01
+    batch.cache.v_scale[batch.tables[0, 28].long()] = 0.02
+    q, scale = queries_of(queries, 4, dim), dim ** -0.5
+    y = T.attention(q, batch.cache, tables.cuda(), whole([held + over]), starts=whole([0, queries]), max_queries=queries)
+    want, bound = defined(q, batch.cache, tables, [held + over], [0, queries], scale)
+    assert torch.all((y.double().cpu() - want).abs() <= bound)
