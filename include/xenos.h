@@ -304,7 +304,8 @@ xenos_status xenos_cache_read(const xenos_cache* cache, int n_tokens, const long
  *   out[t][h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * q[t][h] . k_j - max),   over the keys that t sees, in head h / (heads / cache heads) of the cache.
  * Sequence b has lengths[b] tokens of its own behind the shared prefix, page table[b * table_stride + i] holding tokens i * page_tokens and on; its
  * queries, rows starts[b] .. starts[b + 1] - 1 of q (starts NULL: row b), are the last of those tokens: query i of m sees the whole
- * prefix and the sequence's tokens up to lengths[b] - m + i.  The prefix (prefix_length tokens in the pages of d_prefix_table; 0: none) is read once for all sequences.
+ * prefix and the sequence's tokens up to lengths[b] - m + i.  Rows of q before starts[0] and from starts[n_seqs] on (the padding of a step of fixed size) see
+ * the prefix alone.  The prefix (prefix_length tokens in the pages of d_prefix_table; 0: none) is read once for all sequences.
  * A query that sees nothing gets zeros.  Tokens beyond the table, and those of a page that is none of the cache's, are not seen; a length beyond the table still says which query is which.
  * q and out: element (t, h, d) at t * token_stride + h * head_stride + d, bf16 (the only type: the keys are 8 bits); out must not overlap q.
  * Sums, maxima and the normaliser are fp32; probabilities are rounded to fp16 (relative to the largest value scale) for the product with the values.

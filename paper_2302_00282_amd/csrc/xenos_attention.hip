@@ -53,6 +53,7 @@ struct Item {
   const int* table;
   int tokens;                                                 // of the segment that its table holds
   int length;                                                 // of a sequence: its last query sees the tokens up to this one
+  int seq, tile;
   int first_query, queries;
   int row0, rows;                                             // first row of the tile; rows of the item in all (queries times the group)
   int begin, end;                                             // keys
@@ -73,6 +74,7 @@ __device__ __forceinline__ Item item_of(const AttentionArgs& a, int at, int tile
   const int tile = s.tiles - 1 - at % s.tiles;
   at /= s.tiles;
   const int part = at % s.parts, seq = at / s.parts;
+  it.seq = seq, it.tile = tile;
   if (it.prefix) {
     it.table = a.prefix_table, it.tokens = it.length = a.prefix_len, it.first_query = 0, it.queries = a.n_queries, it.slot = part;
   } else {
@@ -96,6 +98,21 @@ __device__ __forceinline__ Item item_of(const AttentionArgs& a, int at, int tile
 // The keys of a segment that a query sees, from its first one on.
 __device__ __forceinline__ int seen_by(const Item& it, int query) { return it.prefix ? it.tokens : min(it.tokens, it.length - it.queries + query + 1); }
 
+// The rows of q that no sequence has, before the first one's and behind the last one's, see no keys of their own.  Where there are no pieces to be joined nobody else writes their
+// results: the first tile of the first sequence, and of the last one, does.
+__device__ __forceinline__ void blank_rows(const AttentionArgs& a, const Item& it) {
+  if (it.prefix || it.tile || !a.starts || a.own.parts + a.prefix.parts > 1) return;
+  const int width = a.group * a.c.dim;
+  const auto blank = [&](int from, int to) {
+    for (long long i = (long long)from * width + threadIdx.x; i < (long long)to * width; i += 64 * kWaves) {
+      const int query = (int)(i / width), at = (int)(i - (long long)query * width), h = at / a.c.dim;
+      a.out[query * a.out_token + (it.head * a.group + h) * a.out_head + at - h * a.c.dim] = 0;
+    }
+  };
+  if (it.seq == 0) blank(0, it.first_query);
+  if (it.seq == a.n_seqs - 1) blank(it.first_query + it.queries, a.n_queries);
+}
+
 // Where a block of 16 keys of a segment lies: its first row among the cache's, if it has a page.
 struct Block16 {
   long long row;
@@ -118,6 +135,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_k
   __shared__ float s_state[kWaves / 2][REC][64];
   __shared__ __attribute__((aligned(16))) float s_scale[kWaves][2][kKeys];
   Item it = item_of(a, (int)blockIdx.x, 16);
+  blank_rows(a, it);
   const int step_rows = (it.prefix ? a.prefix : a.own).tiles * 16;
   for (; it.row0 < it.rows; it.row0 += step_rows) {           // (once, unless a sequence has more queries than was said)
     int lane = threadIdx.x & 63, dim = a.c.dim;
@@ -325,6 +343,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
   int* s_ok = (int*)(s_ks + 2);
   _Float16 (*s_vs)[kKeys] = (_Float16 (*)[kKeys])(s_ok + 4);
   Item it = item_of(a, (int)blockIdx.x, 32 * kWaves);
+  blank_rows(a, it);
   const int step_rows = (it.prefix ? a.prefix : a.own).tiles * 32 * kWaves;
   for (; it.row0 < it.rows; it.row0 += step_rows) {           // (once, unless a sequence has more queries than was said)
     int lane = threadIdx.x & 63, dim = a.c.dim;
@@ -559,8 +578,11 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
   __shared__ float s_w[2 * kMostParts];
   __shared__ f32x4_t s_o[256];
-  const int row = (int)blockIdx.x, lane = threadIdx.x & 63, slots = a.own.parts + a.prefix.parts, dim = a.c.dim, lanes = dim / 4, groups = 256 / lanes;
-  const float2* ml = (const float2*)a.part_ml + (long long)row * slots;
+  const int row = (int)blockIdx.x, lane = threadIdx.x & 63, all = a.own.parts + a.prefix.parts, dim = a.c.dim, lanes = dim / 4, groups = 256 / lanes;
+  const float2* ml = (const float2*)a.part_ml + (long long)row * all;
+  const int query = row / a.heads, h = row - query * a.heads;
+  // (a row that no sequence has: its pieces are the prefix's, which come first; nobody wrote others)
+  const int slots = !a.starts || (query >= a.starts[0] && query < a.starts[a.n_seqs]) ? all : a.prefix.parts;
   float m[2], l[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -584,7 +606,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
   __syncthreads();
   const int group = (int)threadIdx.x / lanes, d = ((int)threadIdx.x - group * lanes) * 4;
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-  const float* from = a.part + (long long)row * slots * dim + d;
+  const float* from = a.part + (long long)row * all * dim + d;
   if (group < groups)
     for (int s0 = group; s0 < slots; s0 += 4 * groups) {
       float w[4];
@@ -603,7 +625,6 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
   if ((int)threadIdx.x >= lanes) return;
   for (int g = 1; g < groups; ++g) o += s_o[threadIdx.x + g * lanes];
   const float inv = total == 0.f ? 0.f : 1.f / total;
-  const int query = row / a.heads, h = row - query * a.heads;
   uint16_t* to = a.out + (long long)query * a.out_token + h * a.out_head + d;
   const uint32_t lo = f2bf2(o[0] * inv, o[1] * inv), hi = f2bf2(o[2] * inv, o[3] * inv);
   if (a.vec_out) *(uint2*)to = make_uint2(lo, hi);

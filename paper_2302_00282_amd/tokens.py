@@ -208,7 +208,7 @@ def attention(q: torch.Tensor, cache: KVCache, tables: torch.Tensor, lengths: to
 
     Sequence b has lengths[b] (int32 [sequences]) tokens in the pages tables[b] (int32 [sequences][pages], entries behind its last page are not looked at) behind `prefix_length`
     tokens in the pages `prefix_table` (int32) that all sequences share.  Its queries, rows starts[b] .. starts[b + 1] of q (int32 [sequences + 1]; None: row b alone), are the last of
-    its tokens, already in the cache, and each sees the prefix and the tokens up to itself.  max_queries, max_length: what no sequence exceeds
+    its tokens, already in the cache, and each sees the prefix and the tokens up to itself; rows of q that no sequence has see the prefix alone.  max_queries, max_length: what no sequence exceeds
     (max_length None: what its table holds); they decide how the work is shared out and cost no look at the lengths.  scale: None is 1 / sqrt(dim)."""
     device, dim = cache.device, cache.head_dim
     _check(q, "q", device)

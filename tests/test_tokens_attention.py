@@ -435,3 +435,37 @@ def test_many_queries_of_a_length_beyond_the_table(dim, over):
     y = T.attention(q, batch.cache, tables.cuda(), whole([held + over]), starts=whole([0, queries]), max_queries=queries)
     want, bound = defined(q, batch.cache, tables, [held + over], [0, queries], scale)
     assert torch.all((y.double().cpu() - want).abs() <= bound)
+
+
+def attend_into(q, cache, tables, lengths, starts, prefix_table=None, prefix=0):
+    """The C entry, with a result and a workspace that hold what no call left there."""
+    t, h, d = q.shape
+    tables, lengths, starts = tables.cuda(), whole(lengths), whole(starts)
+    prefix_table = None if prefix_table is None else prefix_table.cuda()
+    out = torch.full_like(q, 7.0)
+    args = X.AttentionArgs(len(lengths), t, h, X.XENOS_BF16, q.data_ptr(), h * d, d, out.data_ptr(), h * d, d, starts.data_ptr(), lengths.data_ptr(), tables.data_ptr(), tables.shape[1],
+                           t, tables.shape[1] * cache.page_tokens, None if prefix_table is None else prefix_table.data_ptr(), prefix, d ** -0.5)
+    need = X.xenos_attention_workspace(cache.desc, args)
+    workspace = torch.full((need // 4 + 4,), 3.0, device="cuda")
+    X.xenos_attention(cache.desc, args, workspace.data_ptr(), need, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    return out
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prefix", [0, 77])
+@pytest.mark.parametrize("long", [False, True])
+@pytest.mark.parametrize("queries,before,behind", [([1, 4, 0, 7], 3, 5), ([70, 1, 3, 33], 1, 40), ([5], 33, 0), ([0, 0, 0, 0], 2, 1), ([2, 1], 0, 1)])
+def test_rows_that_no_sequence_has(queries, before, behind, long, prefix):
+    """The padding of a step of fixed size sees the prefix alone."""
+    lengths = [97, 4, 30, 64][:len(queries)]
+    batch = Batch(lengths, 2, 64, 16, prefix)
+    if long:
+        batch = roomy(batch)
+    starts = [before + s for s in starts_of(queries)]
+    q = queries_of(starts[-1] + behind, 4, 64)
+    table = batch.prefix_table if prefix else None
+    y = attend_into(q, batch.cache, batch.tables, lengths, starts, table, prefix)
+    want, bound = defined(q, batch.cache, batch.tables, lengths, starts, 0.125, table, prefix)
+    assert torch.all((y.double().cpu() - want).abs() <= bound)
+    assert prefix or not (y[:before].any() or y[starts[-1]:].any())
