@@ -308,7 +308,8 @@ xenos_status xenos_cache_read(const xenos_cache* cache, int n_tokens, const long
  * the prefix alone.  The prefix (prefix_length tokens in the pages of d_prefix_table; 0: none) is read once for all sequences.
  * A query that sees nothing gets zeros.  Tokens beyond the table, and those of a page that is none of the cache's, are not seen; a length beyond the table still says which query is which.
  * q and out: element (t, h, d) at t * token_stride + h * head_stride + d, bf16 (the only type: the keys are 8 bits); out must not overlap q.
- * Sums, maxima and the normaliser are fp32; probabilities are rounded to fp16 (relative to the largest value scale) for the product with the values.
+ * Sums, references and the normaliser are fp32; for the product with the values each probability times its value's scale is rounded to fp16, relative to the largest of those that
+ * its own row sees (11 bits, and what is below 2^-21 of the largest to 2^-32 of it): no other rounding before the one to bf16 at the end.
  * max_queries and max_length: no sequence has more queries, or tokens of its own.  They choose how the work is shared out, before the lengths are known to the host;
  * lengths and starts stay on the device, so that a captured graph can be replayed as sequences grow.
  * d_workspace: 16-byte aligned, *bytes of xenos_attention_workspace (which reads no device memory); may be 0. */

@@ -1,11 +1,11 @@
 // Attention of a batch of sequences to the quantised cache, with a prefix they share.
 //
-// Keys pass once, 64 at a time, with the running maximum m and sum l of a softmax per row.  The scores are computed transposed, S^T = K Q^T, so that a lane ends up with
+// Keys pass once, 64 at a time, with a running reference and sum of a softmax per row.  The scores are computed transposed, S^T = K Q^T, so that a lane ends up with
 // 16 neighbouring keys of one row (tile t of a wavefront's four takes key 16 (r / 4) + 4 t + r % 4 as its row r): the maximum is over registers and two exchanges, and the lane's
 // probabilities are, as they lie, the operand of O^T += V^T P^T, whose other operand is what the cache holds for one dimension: 16 keys side by side.
 // With few rows keys and values go from memory to registers as they are, and only the scales round through LDS; with many the wavefronts share both there.  The 8-bit keys become bf16 and the values fp16 without rounding; the keys' scales multiply the scores, the values' the probabilities.
-// Those are rounded to fp16 for the product, after division by the largest value scale so far: eight times as fine as bf16, whose error would be as large as that of the
-// rounding of the result (relative error of the output against 64 bits: 1.7e-3 in place of 2.4e-3), and in range whatever the scales are.
+// Those weights are rounded to fp16 for the product, relative to the row's largest (kHead): eight times as fine as bf16, whose error would be as large as that of the
+// rounding of the result (relative error of the output against 64 bits: 1.7e-3 in place of 2.4e-3), and in range whatever the scales are.  Nothing else is rounded on the way.
 #include <algorithm>
 #include <math.h>
 #include "token_device.h"
@@ -123,9 +123,13 @@ struct Block16 {
   }
 };
 
-// The reference m of a row's exponents follows the row's maximum only when that has grown by more than 2^kSlack: probabilities up to 2^kSlack are as exact, and
-// the exchange of maxima and the rescaling of O are rare.
-constexpr float kSlack = 8.f;
+// A key's weight is its probability times its value's scale, and is rounded to fp16, in steps of 2^-24 at the least; so each row counts weights, and the probabilities' sum l with
+// them, in 2^ref of its own: ref is log2 of the largest weight that the row has seen less kHead, and follows only when a weight passes 2^kSlack (the exchange of maxima and the
+// rescaling of O are then rare).  What a row may not see, or hardly looks at, takes no bits from it, however large its value.
+// A scale counts as 2^-88 at the least here: rows of zeros, whose scale is 2^-107, then leave l at 2^15 2^88 a key, in range, and a weight of 2^-107 still has fp16's 11 bits.
+constexpr float kHead = 7.f, kSlack = 15.f, kLeastScale = 0x1p-88f;
+// log2 of a scale (of v_log_f32's error, some 2^-22, a weight's range is the only thing that depends on it)
+__device__ __forceinline__ float size_of_scale(float s) { return __builtin_amdgcn_logf(fmaxf(fabsf(s), kLeastScale)); }
 
 // Few rows: the wavefronts of a workgroup have the same 16 rows and take turns with the keys; their states meet in LDS at the end.  NB: blocks of 64 dimensions.
 // Bound by the cache's bytes: 16 sequences of 100 to 32768 tokens, 8 heads of 128, 32 of queries: 506 MB in 100 to 109 us, 4.6 to 5 TB/s; all of 32768: 1.1 GB in 206, 5.4 TB/s.
@@ -133,7 +137,7 @@ template <int NB>
 __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_kernel(AttentionArgs a) {
   constexpr int DT = 4 * NB, REC = 4 * DT + 2;              // tiles of 16 dimensions; floats of a lane's state
   __shared__ float s_state[kWaves / 2][REC][64];
-  __shared__ __attribute__((aligned(16))) float s_scale[kWaves][2][kKeys];
+  __shared__ __attribute__((aligned(16))) float s_scale[kWaves][3][kKeys];
   Item it = item_of(a, (int)blockIdx.x, 16);
   blank_rows(a, it);
   const int step_rows = (it.prefix ? a.prefix : a.own).tiles * 16;
@@ -171,7 +175,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_k
     const int end = min(it.end, most);
 
     f32x4_t o[DT];
-    float m = -INFINITY, l = 0.f, unit = 7.5e-37f;            // (o counts in `unit`: the largest scale of a value so far)
+    float ref = -INFINITY, l = 0.f;                           // (o and l count in 2^ref)
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     // The blocks of 16 keys that this lane reads: of keys (for the scores' rows), of values, and of its own key's scales.  Their pages are looked up a step ahead, the keys are
@@ -215,39 +219,34 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_k
       request_keys(key + STEP);
       __builtin_amdgcn_sched_barrier(0);
       // the scales of the step's keys, one a lane, go round through LDS
-      const float known = as.ok && key + lane < it.tokens && scale_v < INFINITY ? scale_v : 0.f;
-      float rescale = 1.f;
-      if (__any(known > unit)) {
-        float big = known;
-#pragma unroll
-        for (int x = 32; x; x >>= 1) big = fmaxf(big, __shfl_xor(big, x));
-        rescale = unit / big;
-        unit = big;
-      }
-      s_scale[wave][0][lane] = scale_k * a.scale2;
-      s_scale[wave][1][lane] = scale_v * __builtin_amdgcn_rcpf(unit);
+      // (a value scale that is no number makes the score one that is none, for the rows that see it; the others multiply it by a probability of 0)
+      const float known = fabsf(scale_v) < INFINITY ? scale_v : 0.f;
+      s_scale[wave][0][lane] = fabsf(scale_v) < INFINITY ? scale_k * a.scale2 : __builtin_nanf("");
+      s_scale[wave][1][lane] = known;
+      s_scale[wave][2][lane] = size_of_scale(known);
       f16x8_t p[2];
       const int seen = at.ok ? limit - key - 16 * g : 0;      // of this lane's 16 keys
       float top = -INFINITY;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const f32x4_t ks = *(const f32x4_t*)&s_scale[wave][0][16 * g + 4 * t];
+        const f32x4_t ks = *(const f32x4_t*)&s_scale[wave][0][16 * g + 4 * t], size = *(const f32x4_t*)&s_scale[wave][2][16 * g + 4 * t];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           s[t][e] = 4 * t + e < seen ? s[t][e] * ks[e] : -INFINITY;
-          top = fmaxf(top, s[t][e]);
+          top = fmaxf(top, s[t][e] + size[e]);
         }
       }
-      float keep = rescale;
-      if (__any(top > m + kSlack)) {
+      float keep = 1.f;
+      if (__any(top > ref + kSlack)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float to = fmaxf(m, top), factor = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.f : to));
-        m = to;
-        l *= factor;
-        keep *= factor;
+        if (top > ref + kSlack) {
+          keep = __builtin_amdgcn_exp2f(ref - (top - kHead));
+          ref = top - kHead;
+          l *= keep;
+        }
       }
-      const float base = m == -INFINITY ? 0.f : m;
+      const float base = ref == -INFINITY ? 0.f : ref;
       float sum = 0.f;
       u32x4_t w[2];
 #pragma unroll
@@ -258,7 +257,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_k
         for (int e = 0; e < 4; ++e) {
           const float x = __builtin_amdgcn_exp2f(s[t][e] - base);
           sum += x;
-          pv[e] = 4 * t + e < seen ? x * vs[e] : 0.f;        // (a scale that was never written may be anything)
+          pv[e] = x * vs[e];
         }
         w[t >> 1][2 * (t & 1)] = f2h2(pv[0], pv[1]);
         w[t >> 1][2 * (t & 1) + 1] = f2h2(pv[2], pv[3]);
@@ -279,23 +278,21 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_k
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] *= unit;
     // the states two by two, the upper ones' into the lower ones'
 #pragma unroll
     for (int half = kWaves / 2; half; half >>= 1) {
       if (wave >= half && wave < 2 * half) {
         float (*to)[64] = s_state[wave - half];
-        to[0][lane] = m, to[1][lane] = l;
+        to[0][lane] = ref, to[1][lane] = l;
 #pragma unroll
         for (int d = 0; d < 4 * DT; ++d) to[2 + d][lane] = o[d >> 2][d & 3];
       }
       __syncthreads();
       if (wave < half) {
         float (*from)[64] = s_state[wave];
-        const float om = from[0][lane], top = fmaxf(m, om), base = top == -INFINITY ? 0.f : top;
-        const float mine = __builtin_amdgcn_exp2f(m - base), other = __builtin_amdgcn_exp2f(om - base);
-        m = top;
+        const float theirs = from[0][lane], top = fmaxf(ref, theirs), base = top == -INFINITY ? 0.f : top;
+        const float mine = __builtin_amdgcn_exp2f(ref - base), other = __builtin_amdgcn_exp2f(theirs - base);
+        ref = top;
         l = l * mine + from[1][lane] * other;
 #pragma unroll
         for (int d = 0; d < 4 * DT; ++d) o[d >> 2][d & 3] = o[d >> 2][d & 3] * mine + from[2 + d][lane] * other;
@@ -308,8 +305,8 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_k
       if (row >= it.rows) continue;
       if (slots > 1) {
         const long long at = ((long long)(it.first_query + query) * a.heads + h) * slots + it.slot;
-        if (g == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m, l);
-        if (m == -INFINITY && l == 0.f) continue;          // (nothing seen: its sums are not looked at)
+        if (g == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(ref, l);
+        if (ref == -INFINITY && l == 0.f) continue;          // (nothing seen: its sums are not looked at)
 #pragma unroll
         for (int d = 0; d < DT; ++d)
           if (16 * d < dim) *(f32x4_t*)(a.part + at * dim + 16 * d + 4 * g) = o[d];
@@ -334,14 +331,14 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_k
 // neighbouring keys at a time, an operand of O^T += V^T P^T as it is.
 // Bound by the vector instructions beside the products (the softmax's, a dozen a score, and the conversions): a prompt of 4097, 20 heads of 128 on 4: 86 GFLOP in 143 to 166 us, 520 to 600 TFLOP/s;
 // 512 rows to 16384 shared keys on 4 heads of 128: 17 GFLOP in 37 us.
-// The values carry their scales here (relative to the largest so far, in fp16), once for all rows.
+// Whether a weight may pass 2^kSlack is judged by the largest scale of a step, whoever sees it; only if it may are the scales of the keys that a row sees looked at one by one.
 template <int NB>
 __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_kernel(AttentionArgs a) {
   constexpr int DT = 2 * NB, KP = 128 * NB + 16, VP = 2 * kKeys + 16, KB = kKeys * KP, VB = 64 * NB * VP, CH = 4 * NB;   // pitches (odd numbers of 16-byte places), buffers in bytes
   extern __shared__ __attribute__((aligned(16))) unsigned char s_kv[];
   float (*s_ks)[kKeys] = (float (*)[kKeys])(s_kv + 2 * (KB + VB));
   int* s_ok = (int*)(s_ks + 2);
-  _Float16 (*s_vs)[kKeys] = (_Float16 (*)[kKeys])(s_ok + 4);
+  float (*s_vs)[kKeys] = (float (*)[kKeys])(s_ok + 4);
   Item it = item_of(a, (int)blockIdx.x, 32 * kWaves);
   blank_rows(a, it);
   const int step_rows = (it.prefix ? a.prefix : a.own).tiles * 32 * kWaves;
@@ -381,7 +378,8 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
-    float m = -INFINITY, l = 0.f, unit = 7.5e-37f;
+    float ref = -INFINITY, l = 0.f;                           // (o and l count in 2^ref)
+    float most_scale = kLeastScale, room = 0.f;               // no value of the step has a larger scale; exponents up to which no weight of it passes 2^kSlack
 
     // ---- a step's keys and values on their way: 16 bytes of a key (chunk c of key j), 16 keys of a dimension, the scales of key `lane`
     const int vr = lane & 15, vg = lane >> 4;
@@ -408,7 +406,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
       for (int i = 0; i < NB; ++i) raw_v[i] = *(const u32x4_t*)(v + (16 * (wave * NB + i) < dim ? 256 * (wave * NB + i) : 0));
       scale_k = a.c.k_scale[row + vr], scale_v = a.c.v_scale[row + vr];
     };
-    // they become operands in buffer b; returns what o is to be multiplied by, since it counts in `unit`
+    // they become operands in buffer b
     const auto store = [&](int b) {
       unsigned char *k = s_kv + b * (KB + VB), *v = k + KB;
 #pragma unroll
@@ -417,37 +415,32 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
         *(bf16x8_t*)(k + j * KP + 32 * c) = whole8(raw_k[i][0], raw_k[i][1]);
         *(bf16x8_t*)(k + j * KP + 32 * c + 16) = whole8(raw_k[i][2], raw_k[i][3]);
       }
-      const float known = raw_ok && raw_key + lane < it.tokens && scale_v < INFINITY ? scale_v : 0.f;
-      float rescale = 1.f;
-      if (__any(known > unit)) {                              // (the same for every wavefront)
-        float big = known;
+      // (a value scale that is no number makes the score one that is none: for the rows that see it; the others multiply it by a probability of 0)
+      const bool number = fabsf(scale_v) < INFINITY;
+      const float size = raw_ok && raw_key + lane < it.tokens && number ? fabsf(scale_v) : 0.f;
+      if (__any(size > most_scale)) {                         // (the same for every wavefront)
+        most_scale = size;
 #pragma unroll
-        for (int x = 32; x; x >>= 1) big = fmaxf(big, __shfl_xor(big, x));
-        rescale = unit / big;
-        unit = big;
-      }
-      s_vs[wave][lane] = (_Float16)(known * __builtin_amdgcn_rcpf(unit));    // (this wavefront's own: they go round its lanes)
-      f16x8_t by[2];
-#pragma unroll
-      for (int p = 0; p < 2; ++p) by[p] = *(const f16x8_t*)&s_vs[wave][16 * vg + 8 * p];
+        for (int x = 32; x; x >>= 1) most_scale = fmaxf(most_scale, __shfl_xor(most_scale, x));
+      } else if (!__any(size > most_scale * 0.0625f)) most_scale = fmaxf(most_scale * 0.0625f, kLeastScale);
+      room = kSlack - size_of_scale(most_scale);
 #pragma unroll
       for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int p = 0; p < 2; ++p) *(f16x8_t*)(v + (16 * (wave * NB + i) + vr) * VP + 32 * vg + 16 * p) = half8(raw_v[i][2 * p], raw_v[i][2 * p + 1]) * by[p];
-      if (wave == 0) {                                        // (a value scale that is no number makes the score one that is none: for the rows that see it)
-        s_ks[b][lane] = scale_v < INFINITY ? scale_k * a.scale2 : __builtin_nanf("");
+        for (int p = 0; p < 2; ++p) *(f16x8_t*)(v + (16 * (wave * NB + i) + vr) * VP + 32 * vg + 16 * p) = half8(raw_v[i][2 * p], raw_v[i][2 * p + 1]);
+      if (wave == 0) {
+        s_ks[b][lane] = number ? scale_k * a.scale2 : __builtin_nanf("");
+        s_vs[b][lane] = number ? scale_v : 0.f;
         const uint64_t there = __ballot(raw_ok && vr == 0);
         if (lane == 0) s_ok[b] = (int)((there & 1) | (there >> 15 & 2) | (there >> 30 & 4) | (there >> 45 & 8));
       }
-      return rescale;
     };
 
-    float pending = 1.f;                                      // what o is multiplied by before the next step's product
     __syncthreads();
     if (it.begin < end) {
       look_up(it.begin);
       request(it.begin);
-      pending = store(0);
+      store(0);
       look_up(it.begin + kKeys);
       request(it.begin + kKeys);
     }
@@ -469,10 +462,11 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
             if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (else the operands of all products are read at once, and registers spill)
           }
         }
-        // exponents relative to m (to 0 before a first maximum), in place of the scores
+        // exponents relative to ref (to 0 before a first weight), in place of the scores
         const int ok = s_ok[b];
         const bool open = key + kKeys <= least && __builtin_amdgcn_readfirstlane(ok) == 15;
-        float base = m == -INFINITY ? 0.f : m, top = -INFINITY;
+        const float base = ref == -INFINITY ? 0.f : ref;
+        float top = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -495,23 +489,29 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[t][e]), s[t][e + 1]);
-        float keep = pending;
-        pending = 1.f;
-        if (__any(top > (m == -INFINITY ? -INFINITY : kSlack))) {
-          top = fmaxf(top, __shfl_xor(top, 32));
-          const float up = m == -INFINITY ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f);
-          const float factor = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-up);
-          if (m != -INFINITY || top != -INFINITY) m = base + up;
-          l *= factor;
-          keep *= factor;
+        if (__any(top > (ref == -INFINITY ? -INFINITY : room))) {   // (a weight may pass: with the scales of the keys that each row sees)
+          top = -INFINITY;
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[t][e] -= up;
-        }
-        if (__any(keep != 1.f)) {
+            for (int x = 0; x < 4; ++x) {
+              const f32x4_t vs = *(const f32x4_t*)&s_vs[b][32 * t + 16 * (x >> 1) + 8 * half + 4 * (x & 1)];
 #pragma unroll
-          for (int d = 0; d < DT; ++d) o[d] *= keep;
+              for (int e = 0; e < 4; ++e) top = fmaxf(top, s[t][4 * x + e] + size_of_scale(vs[e]));
+            }
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const bool passes = top > (ref == -INFINITY ? -INFINITY : kSlack);
+          if (__any(passes)) {
+            const float up = passes ? top - kHead : 0.f, keep = !passes ? 1.f : ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-up);
+            if (passes) ref = base + up;
+            l *= keep;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= keep;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) s[t][e] -= up;
+          }
         }
         float sum = 0.f;
 #pragma unroll
@@ -520,8 +520,9 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const float p0 = __builtin_amdgcn_exp2f(s[t][2 * e]), p1 = __builtin_amdgcn_exp2f(s[t][2 * e + 1]);
+            const float2 vs = *(const float2*)&s_vs[b][32 * t + 16 * (e >> 2) + 8 * half + 2 * (e & 3)];
             sum += p0 + p1;
-            w[e >> 2][e & 3] = f2h2(p0, p1);
+            w[e >> 2][e & 3] = f2h2(p0 * vs.x, p1 * vs.y);
           }
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
@@ -534,30 +535,27 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
         l += sum;
       }
       if (key + kKeys < end) {
-        const float next = store(b ^ 1);
-        pending *= next;
+        store(b ^ 1);
         request(key + 2 * kKeys);
       }
     }
     l += __shfl_xor(l, 32);
-    // (o counts in the unit of the last step that was multiplied: `pending` is 1, or there was none after it)
-    const float in = unit * pending;
     if (have) {
       const int slots = a.own.parts + a.prefix.parts;
       if (slots > 1) {
         const long long at = ((long long)(it.first_query + query) * a.heads + h) * slots + it.slot;
-        if (half == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m, l);
-        if (m != -INFINITY || l != 0.f) {                     // (nothing seen: its sums are not looked at)
+        if (half == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(ref, l);
+        if (ref != -INFINITY || l != 0.f) {                     // (nothing seen: its sums are not looked at)
 #pragma unroll
           for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int x = 0; x < 4; ++x)
               if (32 * d + 8 * x < dim)
-                *(f32x4_t*)(a.part + at * dim + 32 * d + 8 * x + 4 * half) = f32x4_t{o[d][4 * x] * in, o[d][4 * x + 1] * in, o[d][4 * x + 2] * in, o[d][4 * x + 3] * in};
+                *(f32x4_t*)(a.part + at * dim + 32 * d + 8 * x + 4 * half) = f32x4_t{o[d][4 * x], o[d][4 * x + 1], o[d][4 * x + 2], o[d][4 * x + 3]};
         }
       } else {
         uint16_t* to = a.out + (long long)(it.first_query + query) * a.out_token + h * a.out_head;
-        const float inv = l == 0.f ? 0.f : in / l;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
