@@ -306,7 +306,8 @@ xenos_status xenos_cache_read(const xenos_cache* cache, int n_tokens, const long
  * queries, rows starts[b] .. starts[b + 1] - 1 of q (starts NULL: row b), are the last of those tokens: query i of m sees the whole
  * prefix and the sequence's tokens up to lengths[b] - m + i.  Rows of q before starts[0] and from starts[n_seqs] on (the padding of a step of fixed size) see
  * the prefix alone.  The prefix (prefix_length tokens in the pages of d_prefix_table; 0: none) is read once for all sequences.
- * A query that sees nothing gets zeros.  Tokens beyond the table, and those of a page that is none of the cache's, are not seen; a length beyond the table still says which query is which.
+ * A query that sees nothing gets zeros, one with an infinity that sees anything NaN.  Tokens beyond the table, and those of a page that is none of the cache's, are not
+ * seen; a length beyond the table still says which query is which.
  * q and out: element (t, h, d) at t * token_stride + h * head_stride + d, bf16 (the only type: the keys are 8 bits); out must not overlap q.
  * Sums, references and the normaliser are fp32; for the product with the values each probability times its value's scale is rounded to fp16, relative to the largest of those that
  * its own row sees (11 bits, and what is below 2^-21 of the largest to 2^-32 of it): no other rounding before the one to bf16 at the end.

@@ -113,6 +113,17 @@ __device__ __forceinline__ void blank_rows(const AttentionArgs& a, const Item& i
   if (it.seq == a.n_seqs - 1) blank(it.first_query + it.queries, a.n_queries);
 }
 
+// Eight values of a query, infinities as NaN: each of its scores is an infinity or a NaN, and their softmax no number; scores that all are -infinity would look like keys that
+// are not seen.
+__device__ __forceinline__ bf16x8_t query8(u32x4_t w) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if ((w[e] & 0x7fffu) == 0x7f80u) w[e] |= 0x40u;
+    if ((w[e] & 0x7fff0000u) == 0x7f800000u) w[e] |= 0x400000u;
+  }
+  return __builtin_bit_cast(bf16x8_t, w);
+}
+
 // Where a block of 16 keys of a segment lies: its first row among the cache's, if it has a page.
 struct Block16 {
   long long row;
@@ -167,7 +178,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_k
               for (int e = 0; e < 8; ++e) w[e >> 1] |= (uint32_t)src[d + e] << (16 * (e & 1));
             }
           }
-          q[b][half] = __builtin_bit_cast(bf16x8_t, w);
+          q[b][half] = query8(w);
         }
     }
 #pragma unroll
@@ -370,7 +381,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
             for (int e = 0; e < 8; ++e) w[e >> 1] |= (uint32_t)src[d + e] << (16 * (e & 1));
           }
         }
-        q[s] = __builtin_bit_cast(bf16x8_t, w);
+        q[s] = query8(w);
       }
     }
     f32x16_t o[DT];

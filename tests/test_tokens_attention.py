@@ -469,3 +469,24 @@ def test_rows_that_no_sequence_has(queries, before, behind, long, prefix):
     want, bound = defined(q, batch.cache, batch.tables, lengths, starts, 0.125, table, prefix)
     assert torch.all((y.double().cpu() - want).abs() <= bound)
     assert prefix or not (y[:before].any() or y[starts[-1]:].any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("long", [False, True])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_a_query_with_an_infinity_has_no_answer(sign, long):
+    """Its scores are infinities: their softmax is no number, however they fall, and not the zeros of a query that sees nothing."""
+    queries = [40, 1, 3]
+    batch = Batch([60, 1, 2], 2, 64, 16)
+    if long:
+        batch = roomy(batch)
+    good = check(batch, queries_of(44, 4, 64), queries)
+    q = queries_of(44, 4, 64)
+    hit = torch.zeros(44, 4, dtype=torch.bool, device="cuda")
+    for t, h, d in ((0, 1, 5), (17, 0, 63), (39, 3, 0), (40, 0, 1), (40, 1, 30), (40, 2, 17), (40, 3, 2), (41, 2, 9), (42, 3, 8), (43, 0, 40)):
+        q[t, h, d] = sign * math.inf
+        hit[t, h] = True
+    hit[41] = False                                             # (the third sequence's first query sees nothing)
+    call = lambda: T.attention(q, batch.cache, batch.tables.cuda(), whole(batch.lengths), starts=whole(starts_of(queries)), max_queries=40)
+    y = call()
+    assert torch.isnan(y[hit]).all() and torch.equal(y[~hit], good[~hit]) and not y[41].any()
