@@ -158,3 +158,47 @@ def test_logprobs_entries_refuse_before_any_launch():
         with pytest.raises(X.XenosError):
             X.xenos_logprobs_workspace(*bad)
     X.xenos_logprobs(**dict(good, rows=0, d_logits=0))
+
+
+def check_strictly(x, targets, top):
+    """As `check`, but what is a number by definition has to be one, and only such numbers are compared."""
+    given, entropy, best, token = T.logprobs(x, targets, top)
+    want, want_entropy, lp = by_definition(x, targets)
+    spread = x.float().cpu().masked_fill(x.cpu() == -INF, 0).abs().amax(-1).double()
+    bound = (x.shape[1] / 64 + 40) * U32 + 6 * U32 * spread
+    for got, expected, b in ((given, want, bound), (entropy, want_entropy, bound * (2 + 2 * spread)), (best, lp.gather(1, token.cpu().long()), bound[:, None].expand(-1, top))):
+        got, finite = got.cpu().double(), torch.isfinite(expected)
+        assert torch.equal(torch.isfinite(got), finite) and torch.equal(got == -INF, expected == -INF)
+        assert torch.all((got - expected).abs()[finite] <= (b + 2 * U32 * expected.abs())[finite])
+    assert torch.equal(token.cpu(), order_of(x, top))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab,top", [(1, 1, 1), (3, 2, 2), (2, 64, 64), (5, 1000, 1), (1, 32000, 5), (7, 4097, 20), (4, 50001, 64), (130, 8193, 8), (1100, 300, 3), (1030, 5000, 0), (1, 200003, 32)])
+def test_logprobs_are_numbers_where_they_are_by_definition(rows, vocab, top, dtype):
+    targets = torch.randint(0, vocab, (rows,), generator=torch.Generator().manual_seed(vocab))
+    targets[rows // 2] = -1
+    check_strictly(drawn(rows, vocab, dtype, rows), targets.cuda(), top)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [600, 5003, 40000])
+def test_masked_and_steep_rows_have_numbers_too(vocab, dtype):
+    x = drawn(10, vocab, dtype, 1)
+    x[0] = 0
+    x[1, 3:] = -INF
+    x[2] = -INF
+    x[2, vocab - 1] = 7.0
+    x[3] = torch.finfo(dtype).min
+    x[4, ::3] = torch.finfo(dtype).min
+    x[5] = torch.arange(vocab) / 8
+    x[6] = -torch.arange(vocab).float() / 8
+    x[7, 100] = 300.0
+    x[8, ::2] = -INF
+    x[9, 0] = torch.finfo(dtype).max
+    targets = torch.tensor([0, 2, vocab - 1, 3, 1, vocab - 1, 0, 100, 1, 0], device="cuda")
+    check_strictly(x, targets, 20)
+    targets = torch.tensor([1, 5, 0, vocab - 1, 0, 0, 1, 101, 0, 1], device="cuda")
+    check_strictly(x, targets, 3)
