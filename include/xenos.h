@@ -311,7 +311,7 @@ xenos_status xenos_cache_read(const xenos_cache* cache, int n_tokens, const long
  * q and out: element (t, h, d) at t * token_stride + h * head_stride + d, bf16 (the only type: the keys are 8 bits); out must not overlap q.
  * Sums, references and the normaliser are fp32; for the product with the values each probability times its value's scale is rounded to fp16, relative to the largest of those that
  * its own row sees (11 bits, and what is below 2^-21 of the largest to 2^-32 of it): no other rounding before the one to bf16 at the end.
- * max_queries and max_length: no sequence has more queries, or tokens of its own.  They choose how the work is shared out, before the lengths are known to the host;
+ * A table holds at most 2^30 tokens.  max_queries and max_length: no sequence has more queries, or tokens of its own.  They choose how the work is shared out, before the lengths are known to the host;
  * lengths and starts stay on the device, so that a captured graph can be replayed as sequences grow.
  * d_workspace: 16-byte aligned, *bytes of xenos_attention_workspace (which reads no device memory); may be 0. */
 typedef struct {

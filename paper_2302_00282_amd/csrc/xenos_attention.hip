@@ -78,10 +78,9 @@ __device__ __forceinline__ Item item_of(const AttentionArgs& a, int at, int tile
   if (it.prefix) {
     it.table = a.prefix_table, it.tokens = it.length = a.prefix_len, it.first_query = 0, it.queries = a.n_queries, it.slot = part;
   } else {
-    const long long held = (long long)a.table_stride * a.c.page;
-    const int n = max(a.lengths[seq], 0);
+    const int held = a.table_stride * a.c.page, n = max(a.lengths[seq], 0);   // (held: at most 2^30)
     it.table = a.tables + (long long)seq * a.table_stride;
-    it.length = n, it.tokens = n < held ? n : (int)held;
+    it.length = n, it.tokens = min(n, held);
     const int lo = a.starts ? a.starts[seq] : seq, hi = a.starts ? a.starts[seq + 1] : seq + 1;
     it.first_query = lo < 0 ? 0 : lo < a.n_queries ? lo : a.n_queries;
     it.queries = hi <= it.first_query ? 0 : (hi < a.n_queries ? hi : a.n_queries) - it.first_query;

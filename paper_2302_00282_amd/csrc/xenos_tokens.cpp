@@ -91,11 +91,13 @@ xenos_status attention_of(const xenos_cache* cache, const xenos_attention_args* 
   if (p->heads % cache->heads) return fail(XENOS_ESHAPE, "%s: %d heads over %d heads of the cache", who, p->heads, cache->heads);
   if (p->max_length > (1 << 30) || p->prefix_length > (1 << 30) || (long long)p->n_queries * p->heads > (1 << 28))
     return fail(XENOS_EUNSUPPORTED, "%s: %d queries of %d heads, %d and %d tokens", who, p->n_queries, p->heads, p->max_length, p->prefix_length);
+  // (the kernels count positions in 32 bits, to a few steps behind the end of what a table holds)
+  if ((long long)p->table_stride * cache->page_tokens > (1 << 30)) return fail(XENOS_EUNSUPPORTED, "%s: tables of %d pages of %d tokens", who, p->table_stride, cache->page_tokens);
   if (p->n_queries > 0 && p->n_seqs == 0) return fail(XENOS_ESHAPE, "%s: %d queries of no sequence", who, p->n_queries);
   if (!p->d_starts && p->n_queries != p->n_seqs) return fail(XENOS_ESHAPE, "%s: %d queries of %d sequences, and no starts", who, p->n_queries, p->n_seqs);
   a.n_seqs = p->n_seqs, a.n_queries = p->n_queries, a.heads = p->heads, a.group = p->heads / cache->heads, a.table_stride = p->table_stride;
   a.prefix_len = p->prefix_length;
-  attention_split(a, std::min(p->max_queries, p->n_queries), (int)std::min<long long>(p->max_length, (long long)p->table_stride * cache->page_tokens));
+  attention_split(a, std::min(p->max_queries, p->n_queries), std::min(p->max_length, p->table_stride * cache->page_tokens));
   const long long own = (long long)a.n_seqs * a.own.tiles * a.own.parts, front = (long long)a.prefix.tiles * a.prefix.parts;
   if ((own + front) * cache->heads > kMostGroups || (long long)p->n_queries * p->heads > 2 * kMostGroups)
     return fail(XENOS_EUNSUPPORTED, "%s: %d queries of %d sequences are more than one launch holds", who, p->n_queries, p->n_seqs);

@@ -490,3 +490,17 @@ def test_a_query_with_an_infinity_has_no_answer(sign, long):
     call = lambda: T.attention(q, batch.cache, batch.tables.cuda(), whole(batch.lengths), starts=whole(starts_of(queries)), max_queries=40)
     y = call()
     assert torch.isnan(y[hit]).all() and torch.equal(y[~hit], good[~hit]) and not y[41].any()
+
+
+def test_tables_of_more_tokens_than_positions_are_refused():
+    """Positions of a sequence are counted in 32 bits, a few steps beyond its end too: lengths, which only the device knows, are held back by the table, so the table is bounded."""
+    p = 256
+    cache = X.Cache(4, 32, 2, 64, p, p, p, p)
+    good = dict(n_seqs=3, n_queries=3, heads=4, dtype=1, d_q=p, q_token_stride=256, q_head_stride=64, d_out=p, out_token_stride=256, out_head_stride=64, d_starts=None, d_lengths=p,
+                d_tables=p, table_stride=1 << 25, max_queries=1, max_length=128, d_prefix_table=None, prefix_length=0, scale=0.125)
+    assert X.xenos_attention_workspace(cache, X.AttentionArgs(**good)) == 0                     # (2^30 tokens)
+    for stride in ((1 << 25) + 1, 1 << 26, (1 << 31) - 1):
+        for call in (lambda a: X.xenos_attention(cache, a, p, 1 << 40), lambda a: X.xenos_attention_workspace(cache, a)):
+            with pytest.raises(X.XenosError) as e:
+                call(X.AttentionArgs(**dict(good, table_stride=stride)))
+            assert e.value.status == X.XENOS_EUNSUPPORTED
