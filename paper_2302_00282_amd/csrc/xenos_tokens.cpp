@@ -1,5 +1,6 @@
 // C-ABI entry points of the operators of a token model's serving step: what a caller hands over is checked here, then launched.
 #include <algorithm>
+#include <utility>
 #include <hip/hip_runtime.h>
 
 #include "status.h"
@@ -79,6 +80,24 @@ xenos_status cache_of(const xenos_cache* c, const char* who, CacheArgs& a) {
     return fail(XENOS_EINVAL, "%s: a cache buffer is not aligned to 16 bytes", who);
   a = CacheArgs{(int8_t*)c->d_k, (int8_t*)c->d_v, c->d_k_scale, c->d_v_scale, c->n_pages, c->page_tokens, c->heads, c->head_dim};
   return XENOS_OK;
+}
+
+// Do any two of tokens x heads rows of `dim` elements, so many elements apart, share one?  (Nested as they are nearly always, the larger stride steps over all rows of the smaller
+// one; else each token is held against those heads of the first one that lie around it.)
+bool rows_overlap(long long tokens, long long heads, long long token_stride, long long head_stride, int dim) {
+  if ((tokens > 1 && token_stride < dim) || (heads > 1 && head_stride < dim)) return true;
+  if (tokens <= 1 || heads <= 1) return false;
+  const auto span = [&](long long n, long long stride) { return (__int128)stride * (n - 1) + dim; };
+  if (head_stride >= span(tokens, token_stride) || token_stride >= span(heads, head_stride)) return false;
+  if (tokens > heads) std::swap(tokens, heads), std::swap(token_stride, head_stride);   // (the loop over the fewer)
+  for (long long t = 1; t < tokens; ++t) {
+    const __int128 at = (__int128)t * token_stride;
+    for (__int128 h = at / head_stride, last = h + 1; h <= last && h < heads; ++h) {
+      const __int128 off = at - h * head_stride;
+      if (off < dim && -off < dim) return true;
+    }
+  }
+  return false;
 }
 
 // Everything of the arguments that can be told without the device's memory.
@@ -199,7 +218,7 @@ xenos_status xenos_attention(const xenos_cache* cache, const xenos_attention_arg
       !aligned(d_workspace, 16))
     return fail(XENOS_EINVAL, "xenos_attention: a buffer is not aligned (the workspace: to 16 bytes)");
   if (p->q_token_stride < 0 || p->q_head_stride < 0 || p->out_token_stride < 0 || p->out_head_stride < 0) return fail(XENOS_ESHAPE, "xenos_attention: negative stride");
-  if ((p->heads > 1 && p->out_head_stride < cache->head_dim) || (p->n_queries > 1 && p->out_token_stride < cache->head_dim))
+  if (rows_overlap(p->n_queries, p->heads, p->out_token_stride, p->out_head_stride, cache->head_dim))
     return fail(XENOS_ESHAPE, "xenos_attention: rows of out overlap (%d values, %lld and %lld apart)", cache->head_dim, p->out_token_stride, p->out_head_stride);
   if (need && (!d_workspace || workspace_bytes < need)) return fail(XENOS_EINVAL, "xenos_attention: a workspace of %zu bytes, %zu are needed", workspace_bytes, need);
   a.q = (const uint16_t*)p->d_q, a.out = (uint16_t*)p->d_out;

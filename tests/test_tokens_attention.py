@@ -1,5 +1,6 @@
 """Attention over the quantised cache against its definition in 64 bits: lengths, pages, shared prefixes, chunks of queries, strides, and what is refused."""
 import math
+import random
 
 import pytest
 import torch
@@ -504,3 +505,28 @@ def test_tables_of_more_tokens_than_positions_are_refused():
             with pytest.raises(X.XenosError) as e:
                 call(X.AttentionArgs(**dict(good, table_stride=stride)))
             assert e.value.status == X.XENOS_EUNSUPPORTED
+
+
+def test_results_that_overlap_are_refused():
+    """Rows of out may lie in any order, but apart: tokens from tokens, heads from heads, and each token's heads from the other tokens'."""
+    p, dim = 256, 64
+    cache = X.Cache(4, 32, 2, dim, p, p, p, p)
+
+    def status(tokens, heads, token_stride, head_stride):
+        a = X.AttentionArgs(n_seqs=tokens, n_queries=tokens, heads=heads, dtype=1, d_q=p, q_token_stride=0, q_head_stride=0, d_out=p, out_token_stride=token_stride, out_head_stride=head_stride,
+                            d_starts=None, d_lengths=p, d_tables=p, table_stride=4, max_queries=1, max_length=128, d_prefix_table=p, prefix_length=40, scale=0.125)
+        with pytest.raises(X.XenosError) as e:
+            X.xenos_attention(cache, a, 0, 0)                                               # (without the workspace it needs: nothing is launched)
+        return e.value.status
+
+    rng = random.Random(7)
+    cases = [(3, 4, 64, 64), (3, 4, 64, 128), (3, 4, 64, 192), (3, 4, 256, 64), (3, 4, 255, 64), (3, 4, 192, 64), (3, 6, 128, 192), (3, 4, 64, 191), (2, 2, 1 << 60, 1 << 61), (4, 4, 1 << 62, 1 << 62),
+             (5, 2, 100, 250), (5, 2, 100, 270)]
+    cases += [(rng.randint(1, 9), 2 * rng.randint(1, 5), rng.randint(64, 700), rng.randint(64, 700)) for _ in range(300)]
+    found = set()
+    for tokens, heads, ts, hs in cases:
+        at = sorted(t * ts + h * hs for t in range(tokens) for h in range(heads))
+        apart = all(b - a >= dim for a, b in zip(at, at[1:]))
+        assert status(tokens, heads, ts, hs) == (X.XENOS_EINVAL if apart else X.XENOS_ESHAPE), (tokens, heads, ts, hs)
+        found.add((apart, min(ts * (tokens - 1), hs * (heads - 1)) + dim <= max(ts, hs)))
+    assert {(True, True), (True, False), (False, False)} <= found                           # (nested or not)
