@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libxenos.so")
 SOURCES = ["xenos_kernels.hip", "xenos_conv3.hip", "xenos_linked.hip", "xenos_unit.hip", "xenos_wave.hip", "xenos_quant.hip",
            "xenos_cache.hip", "xenos_logprobs.hip", "xenos_attention.hip", "xenos_lib.cpp", "xenos_tokens.cpp"]
-HEADERS = ["kernels.h", "token_kernels.h", "token_device.h", "status.h", "device_common.h", "wave_gemm.h", "index_div.h", os.path.join("..", "..", "include", "xenos.h")]
+HEADERS = ["kernels.h", "token_kernels.h", "token_device.h", "status.h", "device_common.h", "per_device.h", "wave_gemm.h", "index_div.h", os.path.join("..", "..", "include", "xenos.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]

@@ -3,10 +3,10 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
-#include <atomic>
 #include <type_traits>
 #include "index_div.h"
 #include "kernels.h"
+#include "per_device.h"
 
 namespace xenos {
 
@@ -169,17 +169,6 @@ __device__ __forceinline__ int tile_div(int n, int d, unsigned mul) {
   if (mul) return (int)host_quotient((unsigned)n, mul);
   asm volatile("" : "+s"(d));                          // (nothing of the division is worked out ahead, for calls that need none)
   return uniform_div(n, d);
-}
-
-// Dynamic LDS of a kernel whose launches differ in their need: its limit is raised once, to all of a unit's memory.  (Raised to what
-// the launch at hand needs, two threads' first launches could leave the smaller limit behind.)
-constexpr int kLdsPerUnit = 160 * 1024;
-template <typename F>
-inline hipError_t raise_lds_limit(F* kernel, std::atomic<bool>& raised) {
-  if (raised.load(std::memory_order_acquire)) return hipSuccess;
-  const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsPerUnit);
-  if (e == hipSuccess) raised.store(true, std::memory_order_release);
-  return e;
 }
 
 constexpr int NT = 256;          // threads per workgroup (4 wavefronts of 64)

@@ -644,7 +644,7 @@ template <int NB>
 int attention_rows(const AttentionArgs& a, bool many, int grid, hipStream_t st) {
   if (!many) attention_kernel<NB><<<grid, 64 * kWaves, 0, st>>>(a);
   else {
-    static std::atomic<bool> raised{false};
+    static PerDevice raised;
     const hipError_t e = raise_lds_limit(attention_tile_kernel<NB>, raised);
     if (e != hipSuccess) return (int)e;
     constexpr int lds = 2 * (kKeys * (128 * NB + 16) + 64 * NB * (2 * kKeys + 16) + 4 * kKeys) + 16 + kWaves * 2 * kKeys;

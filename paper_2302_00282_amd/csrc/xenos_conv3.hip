@@ -291,7 +291,7 @@ __global__ __launch_bounds__(NT, 2) void conv3x3_frag_kernel(const Frag3Args a) 
 
 template <int PB, int WP, int KS, bool ZIG>
 static int launch_frag3_inst(const Frag3Args& w, int grid, hipStream_t st) {
-  static std::atomic<bool> raised{false};
+  static PerDevice raised;
   const hipError_t e = raise_lds_limit(conv3x3_frag_kernel<PB, WP, KS, ZIG>, raised);
   if (e != hipSuccess) return (int)e;
   hipLaunchKernelGGL((conv3x3_frag_kernel<PB, WP, KS, ZIG>), dim3(grid), dim3(NT), (int)frag3_lds(PB, WP, KS), st, w);

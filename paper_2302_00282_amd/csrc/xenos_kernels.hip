@@ -1242,12 +1242,9 @@ __global__ __launch_bounds__(V2_NT) void conv3x3_kernel(const ConvArgs a) {
 
 template <typename T, int MODE, int PWID, int BN, bool PART = false>
 static int launch_conv3x3_pw(const ConvArgs& a, hipStream_t st) {
-  static bool raised = false;
-  if (!raised) {
-    hipError_t e = hipFuncSetAttribute((const void*)conv3x3_kernel<T, MODE, PWID, BN, PART>, hipFuncAttributeMaxDynamicSharedMemorySize, v2_lds_total(BN));
-    if (e != hipSuccess) return (int)e;
-    raised = true;
-  }
+  static PerDevice raised;
+  const hipError_t e = raise_lds_limit(conv3x3_kernel<T, MODE, PWID, BN, PART>, raised, v2_lds_total(BN));
+  if (e != hipSuccess) return (int)e;
   hipLaunchKernelGGL((conv3x3_kernel<T, MODE, PWID, BN, PART>), dim3(a.grid), dim3(V2_NT), v2_lds_total(BN), st, a);
   return (int)hipGetLastError();
 }
@@ -2288,14 +2285,10 @@ static int launch_stem_lds(const ConvArgs& a, int dtype, hipStream_t st) {
 template <typename T, int BM, int BN, int WM, int WN, bool SCALAR, int MODE, bool UNI>
 static int launch_conv_uni(const ConvArgs& a, hipStream_t st) {
   constexpr int lds = lds_conv_bytes<BM, BN>();
-  if (lds > 64 * 1024) {   // more than the default dynamic-LDS limit: raise it once per instantiation
-    static bool raised = false;
-    if (!raised) {
-      hipError_t e = hipFuncSetAttribute((const void*)conv_kernel<T, BM, BN, WM, WN, SCALAR, MODE, false, UNI>,
-                                         hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-      if (e != hipSuccess) return (int)e;
-      raised = true;
-    }
+  if (lds > 64 * 1024) {   // more than the default dynamic-LDS limit
+    static PerDevice raised;
+    const hipError_t e = raise_lds_limit(conv_kernel<T, BM, BN, WM, WN, SCALAR, MODE, false, UNI>, raised, lds);
+    if (e != hipSuccess) return (int)e;
   }
   hipLaunchKernelGGL((conv_kernel<T, BM, BN, WM, WN, SCALAR, MODE, false, UNI>), dim3(a.grid), dim3(NT), lds, st, a);
   return (int)hipGetLastError();
@@ -2555,7 +2548,7 @@ static int launch_dwpw_t(const ConvArgs& a, hipStream_t st) {
       a.tiles_m != (a.M_total + 63) / 64 || a.tiles_n != (a.K + 63) / 64 || a.ntiles != a.tiles_m * a.tiles_n || a.grid < 1 ||
       a.Kred_pad < (a.C + BKE - 1) / BKE * BKE || !a.dw_w || !a.dw_scale || !a.dw_shift || !a.zeros || ((uintptr_t)a.zeros & 15))
     return (int)hipErrorInvalidValue;
-  static std::atomic<bool> raised{false};
+  static PerDevice raised;
   const hipError_t e = raise_lds_limit(dwpw_kernel<T>, raised);
   if (e != hipSuccess) return (int)e;
   hipLaunchKernelGGL((dwpw_kernel<T>), dim3(a.grid < a.ntiles ? a.grid : a.ntiles), dim3(NT), lds, st, a);
@@ -2565,12 +2558,10 @@ static int launch_dwpw_t(const ConvArgs& a, hipStream_t st) {
 template <typename T, int BM, int BN, int WM, int WN, int MODE>
 static int launch_conv_dwpro_inst(const ConvArgs& a, hipStream_t st) {
   constexpr int lds = lds_conv_bytes<BM, BN>();
-  static bool raised = false;
-  if (lds > 64 * 1024 && !raised) {
-    hipError_t e = hipFuncSetAttribute((const void*)conv_kernel<T, BM, BN, WM, WN, false, MODE, true>,
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (lds > 64 * 1024) {
+    static PerDevice raised;
+    const hipError_t e = raise_lds_limit(conv_kernel<T, BM, BN, WM, WN, false, MODE, true>, raised, lds);
     if (e != hipSuccess) return (int)e;
-    raised = true;
   }
   hipLaunchKernelGGL((conv_kernel<T, BM, BN, WM, WN, false, MODE, true>), dim3(a.grid), dim3(NT), lds, st, a);
   return (int)hipGetLastError();

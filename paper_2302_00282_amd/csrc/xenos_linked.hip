@@ -337,7 +337,7 @@ static int launch_pwdw_t(const ConvArgs& a, hipStream_t st) {
   const int positions = ((a.th - 1) * s + 3) * ((a.tw - 1) * s + 3);
   const int lds = pwdw_lds(positions, ESZ);
   if (positions > kPwDwMaxPositions || lds > 160 * 1024) return (int)hipErrorInvalidValue;
-  static std::atomic<bool> raised{false};
+  static PerDevice raised;
   const hipError_t e = raise_lds_limit(pwdw_kernel<T>, raised);
   if (e != hipSuccess) return (int)e;
   ConvArgs b = a;
@@ -734,7 +734,7 @@ __global__ __launch_bounds__(NT, 2) void fire_kernel(const ConvArgs a) {
 
 template <typename T, bool POOL, int TAPS1, int KGS>
 static int launch_fire_kgs(const ConvArgs& a, int lds, hipStream_t st) {
-  static std::atomic<bool> raised{false};
+  static PerDevice raised;
   const hipError_t e = raise_lds_limit(fire_kernel<T, POOL, TAPS1, KGS>, raised);
   if (e != hipSuccess) return (int)e;
   ConvArgs b = a;

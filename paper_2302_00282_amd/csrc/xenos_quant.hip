@@ -459,7 +459,7 @@ __global__ __launch_bounds__(256) void quant_finish_kernel(QuantMatmulArgs a, in
 template <typename T, int WM, int WN, int TM, int TN, int STAGES>
 static int quant_tiles_of(const QuantMatmulArgs& a, int splits, hipStream_t st) {
   constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN, lds = (BM + BN) * 128 * STAGES;
-  static std::atomic<bool> raised{false};
+  static PerDevice raised;
   const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
   const hipError_t e = raise_lds_limit(quant_matmul_kernel<T, WM, WN, TM, TN, STAGES>, raised);
   if (e != hipSuccess) return (int)e;

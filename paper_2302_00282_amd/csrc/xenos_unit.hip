@@ -391,7 +391,7 @@ static int launch_unit_t(const ConvArgs& a, hipStream_t st) {
     return (int)hipErrorInvalidValue;
   const int lds = (int)unit_lds_bytes(a.th, a.tw, s, a.unit_C, a.C, ESZ);
   if (lds > 160 * 1024) return (int)hipErrorInvalidValue;
-  static std::atomic<bool> raised{false};
+  static PerDevice raised;
   const hipError_t e = raise_lds_limit(unit_kernel<T>, raised);
   if (e != hipSuccess) return (int)e;
   ConvArgs b = a;

@@ -350,7 +350,7 @@ int conv_wave_stages(int edge, int steps, int tiles, int esz) {
 
 template <typename T, int NB, bool UNI, bool DIRECT>
 static int launch_conv_wave_inst(const WaveConvArgs& w, int grid, int lds, hipStream_t st) {
-  static std::atomic<bool> raised{false};
+  static PerDevice raised;
   const hipError_t e = raise_lds_limit(conv_wave_kernel<T, NB, UNI, DIRECT>, raised);
   if (e != hipSuccess) return (int)e;
   hipLaunchKernelGGL((conv_wave_kernel<T, NB, UNI, DIRECT>), dim3(std::min((uint32_t)grid, w.tiles)), dim3(NT), lds, st, w);
@@ -401,7 +401,7 @@ size_t pwdw_wave_lds(const ConvArgs& a, int esz) {
 
 template <typename T, bool DIRECT>
 static int launch_pwdw_wave_inst(const WavePwDwArgs& w, int grid, int lds, hipStream_t st) {
-  static std::atomic<bool> raised{false};
+  static PerDevice raised;
   const hipError_t e = raise_lds_limit(pwdw_wave_kernel<T, DIRECT>, raised);
   if (e != hipSuccess) return (int)e;
   hipLaunchKernelGGL((pwdw_wave_kernel<T, DIRECT>), dim3(std::min((uint32_t)grid, w.tiles)), dim3(NT), lds, st, w);
