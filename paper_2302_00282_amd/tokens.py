@@ -3,7 +3,7 @@ attention that reads it, and what is read from the logits.
 
 Each function checks its tensors, allocates what it returns, and makes one call of the C ABI (include/xenos.h) on torch's current
 stream of the tensors' device; nothing synchronises.  The kernels are the library's own: there is no CPU path.  Forward passes only: what
-they return carries no gradient, and an input that asks for one is refused.
+they return carries no gradient, and an input that asks for one, or has a tangent, is refused.
 """
 from __future__ import annotations
 
@@ -11,6 +11,7 @@ import math
 from typing import Optional, Tuple
 
 import torch
+import torch.autograd.forward_ad as _forward
 
 from . import xenos as X
 
@@ -39,6 +40,8 @@ def _check(t: torch.Tensor, name: str, device: Optional[int], dtype=None, shape=
         _refuse(X.XENOS_ESHAPE, f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
     if t.requires_grad and torch.is_grad_enabled():
         _refuse(X.XENOS_EUNSUPPORTED, f"{name} requires a gradient: these operators have no backward pass")
+    if _forward._current_level >= 0 and t.is_floating_point() and _forward.unpack_dual(t).tangent is not None:
+        _refuse(X.XENOS_EUNSUPPORTED, f"{name} has a tangent: these operators have no derivatives")
     return t
 
 

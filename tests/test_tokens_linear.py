@@ -239,3 +239,21 @@ def test_linear_entries_refuse_before_any_launch():
             X.xenos_linear_workspace(*bad)
     X.xenos_linear(X.LinearArgs(**dict(good, rows=0, d_x=None)))
     X.xenos_linear(X.LinearArgs(**dict(good, out_c=0, d_out=None)), p, need)
+
+
+@pytest.mark.gpu
+def test_an_input_with_a_tangent_is_refused():
+    """Forward-mode derivatives are asked for without requires_grad: they are refused like the others, not dropped."""
+    import torch.autograd.forward_ad as forward
+    w, w_scale = T.quantize_rows(drawn(16, 100, torch.float32, 2).cuda())
+    x, b = drawn(4, 100, torch.float32, 1).cuda(), torch.ones(16, device="cuda")
+    want = T.linear(x, w, w_scale, bias=b)
+    with forward.dual_level():
+        dual, dual_b = forward.make_dual(x, torch.ones_like(x)), forward.make_dual(b, torch.ones_like(b))
+        for call in (lambda: T.linear(dual, w, w_scale), lambda: T.linear(x, w, w_scale, bias=dual_b), lambda: T.quantize_rows(dual), lambda: T.logprobs(dual)):
+            with pytest.raises(X.XenosError) as e:
+                call()
+            assert e.value.status == X.XENOS_EUNSUPPORTED and "tangent" in str(e.value)
+        assert torch.equal(T.linear(x, w, w_scale, bias=b), want)               # (within a level, but without tangents)
+        assert torch.equal(T.linear(forward.unpack_dual(dual).primal, w, w_scale, bias=b), want)
+    assert torch.equal(T.linear(x, w, w_scale, bias=b), want)
