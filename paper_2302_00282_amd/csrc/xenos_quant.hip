@@ -58,8 +58,25 @@ __device__ __forceinline__ uint2 packed8(const RowStep& step, const float* v) {
   const auto four = [](const uint32_t* w) { return __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0c0c0400u), __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0400u), 0x05040100u); };
   return make_uint2(four(u), four(u + 4));
 }
-__device__ __forceinline__ float row_scale(const QuantRowsArgs& a, const RowStep& step, float sq) {
-  return a.gamma ? step.scale() * (1.f / sqrtf(sq / (float)a.cols + a.eps)) : step.scale();
+// What a row's values are multiplied by before they are squared: 1, and only where that sum has overflowed, or lost bits below the least normal number that eps does not
+// cover, a power of 2 that brings every value's square into range.  (Such a row is read once more.)
+__device__ __forceinline__ float square_unit(const QuantRowsArgs& a, float sq) {
+  return !a.gamma ? 1.f : sq == INFINITY ? 0x1p-75f : sq / (float)a.cols + a.eps < 0x1p-70f ? 0x1p64f : 1.f;
+}
+// This thread's share of a row's squares, elements `first` to `first` + 7 and so on in steps of `step`, in that unit.
+template <typename T>
+__device__ __forceinline__ float squares(const QuantRowsArgs& a, const T* row, int first, int step, float by) {
+  float sq = 0.f;
+  for (int i = first; i < a.cols; i += step) {
+    float f[8];
+    load8<T>(row, i, a.cols, a.vec, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sq += (f[e] * by) * (f[e] * by);
+  }
+  return sq;
+}
+__device__ __forceinline__ float row_scale(const QuantRowsArgs& a, const RowStep& step, float sq, float by) {
+  return a.gamma ? step.scale() * (1.f / sqrtf(sq / (float)a.cols + a.eps * by * by)) * by : step.scale();
 }
 
 // One workgroup per row: q = rint(x g 127 / a), a = max|x g|, scale = a / 127 [/ rms(x)].  The norm's factor is one number per row: it
@@ -111,7 +128,16 @@ __global__ __launch_bounds__(1024) void quant_rows_kernel(QuantRowsArgs a) {
         *(uint2*)(q + i) = packed8(unit, v[0]);
       }
     }
-    if (threadIdx.x == 0) a.scale[at] = row_scale(a, unit, sq);
+    const float by = square_unit(a, sq);
+    if (by != 1.f) {                                          // (the same for every thread)
+      sq = wave_sum(squares(a, row, (int)threadIdx.x * 8, step, by));
+      __syncthreads();
+      if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sq;
+      __syncthreads();
+      sq = 0.f;
+      for (int w = 0; w < waves; ++w) sq += s_sum[w];
+    }
+    if (threadIdx.x == 0) a.scale[at] = row_scale(a, unit, sq, by);
     __syncthreads();                                          // (s_max and s_sum are free again)
   }
 }
@@ -232,10 +258,12 @@ __device__ __forceinline__ void quant_into_lds(const QuantRowsArgs& a, int8_t* q
       times_gamma(a, i, f, v, [](float) {});
       *(uint2*)(q + r * a.pitch + i) = packed8(step, v);
     }
-    if (piece == 0 && lane == 0) {
+    if (piece == 0) {
       float sq = 0.f;
       for (int w = 0; w < share; ++w) sq += s_sum[r][w];
-      scale[r] = row_scale(a, step, sq);
+      const float by = square_unit(a, sq);
+      if (by != 1.f) sq = wave_sum(squares(a, row, lane * 8, 512, by));
+      if (lane == 0) scale[r] = row_scale(a, step, sq, by);
     }
   }
   __syncthreads();

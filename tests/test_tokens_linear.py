@@ -257,3 +257,30 @@ def test_an_input_with_a_tangent_is_refused():
         assert torch.equal(T.linear(x, w, w_scale, bias=b), want)               # (within a level, but without tangents)
         assert torch.equal(T.linear(forward.unpack_dual(dual).primal, w, w_scale, bias=b), want)
     assert torch.equal(T.linear(x, w, w_scale, bias=b), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cols", [100, 1000, 3001, 9000, 20000])
+def test_norm_of_rows_whose_squares_leave_the_range(cols, dtype):
+    """The norm's factor of a row is that of its definition where the sum of its squares overflows, or underflows with eps as small."""
+    x = drawn(8, cols, torch.float32, 3, False).clamp(-3, 3)
+    x[0] *= 1e20
+    x[1] *= 1e38
+    x[2] *= 1e-10
+    x[3, 7] = 2.9e38
+    x[4] *= 1e18
+    x[6] *= 1e-21
+    x[7] *= 1e-29
+    x, gamma = x.to(dtype), torch.rand(cols, generator=torch.Generator().manual_seed(1)) * 0.9 + 0.05
+    w, w_scale = T.quantize_rows(drawn(24, cols, torch.float32, 2, False).cuda())
+    for eps in (1e-5, 0.0):
+        q, scale = T.quantize_rows(x.cuda(), gamma.cuda(), eps)
+        want, want_scale = rows_by_definition(x, gamma, eps)
+        assert torch.equal(q[:, :cols].cpu().float(), want)
+        bound = (cols / 256 + 36) * U32 * want_scale
+        assert torch.all((scale.cpu().double() - want_scale).abs() <= bound)
+        for rows in (1, 3, 8):                                  # (of short rows: as every workgroup of the product does it)
+            y = T.linear(x[:rows].cuda(), w, w_scale, gamma=gamma.cuda(), eps=eps)
+            y_want, size = product_by_definition(q[:rows], want_scale[:rows].cuda(), w, w_scale, None, None, False)
+            assert torch.all((y.double() - y_want).abs() <= (5.1 + cols / 256 + 36) * U32 * size + (U16 * y_want.abs() if dtype == torch.bfloat16 else 0) * 1.01 + 1e-38)
