@@ -19,6 +19,7 @@ from . import xenos as X
 # stream's handle is asked for without making a Stream object of it (0.1 us in place of 2 us).
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _DTYPE = {torch.float32: X.XENOS_F32, torch.bfloat16: X.XENOS_BF16}
+_INT_MAX = (1 << 31) - 1      # (sizes are ints of the C ABI, and ctypes keeps the lower bits of a larger one)
 
 
 def _refuse(status: int, message: str):
@@ -43,6 +44,10 @@ def _check(t: torch.Tensor, name: str, device: Optional[int], dtype=None, shape=
     if _forward._current_level >= 0 and t.is_floating_point() and _forward.unpack_dual(t).tangent is not None:
         _refuse(X.XENOS_EUNSUPPORTED, f"{name} has a tangent: these operators have no derivatives")
     return t
+
+
+def _too_many(what: str):
+    _refuse(X.XENOS_EUNSUPPORTED, f"{what}: sizes of at most {_INT_MAX}")
 
 
 def _given(t: Optional[torch.Tensor], name: str, device: int, shape, dtype=torch.float32) -> Optional[torch.Tensor]:
@@ -83,6 +88,8 @@ def quantize_rows(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, eps: fl
     if x.dim() != 2 or x.shape[1] == 0:
         _refuse(X.XENOS_ESHAPE, f"x is {tuple(x.shape)}, not rows x columns")
     rows, cols = x.shape
+    if rows > _INT_MAX or cols > _INT_MAX:
+        _too_many(f"x is {rows} x {cols}")
     x, gamma = _rows(x), _given(gamma, "gamma", device, (cols,))
     q, scale = x.new_empty((rows, quant_pitch(cols)), dtype=torch.int8), x.new_empty(rows, dtype=torch.float32)
     _launch(device, X.xenos_quant_rows, x.data_ptr(), _DTYPE[x.dtype], rows, cols, x.stride(0), _address(gamma), eps, q.data_ptr(), scale.data_ptr())
@@ -93,6 +100,8 @@ def _weights(w: torch.Tensor, device: int, cols: int) -> torch.Tensor:
     _check(w, "w", device, torch.int8)
     if w.dim() != 2 or w.shape[1] != quant_pitch(cols):
         _refuse(X.XENOS_ESHAPE, f"w is {tuple(w.shape)}, not rows of {quant_pitch(cols)} bytes for {cols} columns")
+    if w.shape[0] > _INT_MAX:
+        _too_many(f"w is {tuple(w.shape)}")
     return w.contiguous()
 
 
@@ -104,6 +113,8 @@ def quant_matmul(q: torch.Tensor, scale: torch.Tensor, w: torch.Tensor, w_scale:
         _refuse(X.XENOS_ESHAPE, f"q is {tuple(q.shape)}, not rows of {quant_pitch(cols)} bytes for {cols} columns")
     if dtype not in _DTYPE:
         _refuse(X.XENOS_EUNSUPPORTED, f"{dtype}: float32 and bfloat16 are supported")
+    if q.shape[0] > _INT_MAX or cols > _INT_MAX:
+        _too_many(f"q is {tuple(q.shape)}")
     q, w = q.contiguous(), _weights(w, device, cols)
     rows, out_c = q.shape[0], w.shape[0]
     scale, w_scale, bias = _given(scale, "scale", device, (rows,)), _given(w_scale, "w_scale", device, (out_c,)), _given(bias, "bias", device, (out_c,))
@@ -125,6 +136,8 @@ def linear(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, bias: Opt
     if len(shape) == 0 or shape[-1] == 0:
         _refuse(X.XENOS_ESHAPE, f"x is {tuple(shape)}, without columns")
     cols = shape[-1]
+    if cols > _INT_MAX or x.numel() // cols > _INT_MAX:
+        _too_many(f"x is {tuple(shape)}")
     w = _weights(w, device, cols)
     out_c = w.shape[0]
     if residual is not None:
@@ -154,6 +167,8 @@ class KVCache:
         if k.dim() != 4:
             _refuse(X.XENOS_ESHAPE, f"k is {tuple(k.shape)}, not pages x heads x tokens x dimensions")
         n, heads, page, dim = k.shape
+        if max(k.shape) > _INT_MAX:
+            _too_many(f"k is {tuple(k.shape)}")
         _check(v, "v", device, torch.int8, (n, heads, page // 16, dim, 16))
         _check(k_scale, "k_scale", device, torch.float32, (n, heads, page))
         _check(v_scale, "v_scale", device, torch.float32, (n, heads, page))
@@ -181,6 +196,8 @@ class KVCache:
         shape = k.shape
         if len(shape) != 3 or shape[1] != self.heads or shape[2] != self.head_dim:
             _refuse(X.XENOS_ESHAPE, f"k is {tuple(shape)}, not tokens x {self.heads} x {self.head_dim}")
+        if shape[0] > _INT_MAX:
+            _too_many(f"k is {tuple(shape)}")
         _check(v, "v", self.device, k.dtype, shape)
         slots = _given(slots, "slots", self.device, shape[:1], torch.int64)
         if k.stride(2) != 1:
@@ -195,6 +212,8 @@ class KVCache:
         _check(slots, "slots", self.device, torch.int64)
         if slots.dim() != 1:
             _refuse(X.XENOS_ESHAPE, f"slots is {tuple(slots.shape)}, not a list")
+        if slots.shape[0] > _INT_MAX:
+            _too_many(f"slots is {tuple(slots.shape)}")
         if dtype not in _DTYPE:
             _refuse(X.XENOS_EUNSUPPORTED, f"{dtype}: float32 and bfloat16 are supported")
         slots = slots.contiguous()
@@ -220,10 +239,14 @@ def attention(q: torch.Tensor, cache: KVCache, tables: torch.Tensor, lengths: to
         _refuse(X.XENOS_EUNSUPPORTED, f"q is {q.dtype}: bfloat16 is supported")
     if len(shape) != 3 or shape[2] != dim or shape[1] == 0 or shape[1] % cache.heads:
         _refuse(X.XENOS_ESHAPE, f"q is {tuple(shape)}, not queries x a multiple of {cache.heads} heads x {dim}")
-    tables = _given(tables, "tables", device, None, torch.int32)
     if len(ts) != 2:
         _refuse(X.XENOS_ESHAPE, f"tables is {tuple(ts)}, not sequences x pages")
     n_seqs = ts[0]
+    if max_length is None:
+        max_length = ts[1] * cache.page_tokens
+    if max(shape[0], shape[1], n_seqs, ts[1], max_length, prefix_length) > _INT_MAX:
+        _too_many(f"{shape[0]} queries of {shape[1]} heads, tables of {tuple(ts)}, up to {max_length} tokens behind {prefix_length}")
+    tables = _given(tables, "tables", device, None, torch.int32)
     lengths, starts = _given(lengths, "lengths", device, (n_seqs,), torch.int32), _given(starts, "starts", device, (n_seqs + 1,), torch.int32)
     if starts is None and shape[0] != n_seqs:
         _refuse(X.XENOS_ESHAPE, f"{shape[0]} queries of {n_seqs} sequences, and no starts")
@@ -238,7 +261,7 @@ def attention(q: torch.Tensor, cache: KVCache, tables: torch.Tensor, lengths: to
         _refuse(X.XENOS_ESHAPE, "the rows of out are not contiguous")
     qs, os = q.stride(), out.stride()
     args = X.AttentionArgs(n_seqs, shape[0], shape[1], X.XENOS_BF16, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1], _address(starts), lengths.data_ptr(),
-                           tables.data_ptr(), ts[1], max_queries, ts[1] * cache.page_tokens if max_length is None else max_length, _address(prefix_table), prefix_length,
+                           tables.data_ptr(), ts[1], min(max_queries, shape[0]), max_length, _address(prefix_table), prefix_length,
                            1.0 / math.sqrt(dim) if scale is None else scale)
     need = X.xenos_attention_workspace(cache.desc, args)
     workspace = q.new_empty(need, dtype=torch.uint8) if need else None
@@ -256,6 +279,8 @@ def logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: 
     if logits.dim() != 2 or logits.shape[1] == 0:
         _refuse(X.XENOS_ESHAPE, f"logits is {tuple(logits.shape)}, not positions x tokens")
     rows, vocab = logits.shape
+    if rows > _INT_MAX or vocab > _INT_MAX:
+        _too_many(f"logits is {rows} x {vocab}")
     if not 0 <= top <= X.XENOS_TOP_MAX:
         _refuse(X.XENOS_EUNSUPPORTED, f"the best {top} tokens (at most {X.XENOS_TOP_MAX})")
     if top > vocab:

@@ -530,3 +530,21 @@ def test_results_that_overlap_are_refused():
         assert status(tokens, heads, ts, hs) == (X.XENOS_EINVAL if apart else X.XENOS_ESHAPE), (tokens, heads, ts, hs)
         found.add((apart, min(ts * (tokens - 1), hs * (heads - 1)) + dim <= max(ts, hs)))
     assert {(True, True), (True, False), (False, False)} <= found                           # (nested or not)
+
+
+@pytest.mark.gpu
+def test_counts_that_pass_31_bits():
+    batch = Batch([33], 2, 64, 16, 20)
+    q, tables, lengths = queries_of(1, 4, 64), batch.tables.cuda(), whole([33])
+    front = dict(prefix_table=batch.prefix_table.cuda()[:1].expand(1 << 29), prefix_length=(1 << 32) + 5)
+    far = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for call in (lambda: T.attention(q, batch.cache, tables, lengths, **front), lambda: T.attention(q, batch.cache, tables, lengths, max_length=(1 << 32) + 33),
+                 lambda: T.attention(q.expand((1 << 32) + 1, 4, 64), batch.cache, tables, lengths, starts=whole([0, 1])),
+                 lambda: T.attention(q, batch.cache, far.expand((1 << 32) + 1, 1), far.expand((1 << 32) + 1), starts=far.expand((1 << 32) + 2)),
+                 lambda: batch.cache.write(q[:, :2].expand((1 << 32) + 1, 2, 64), q[:, :2].expand((1 << 32) + 1, 2, 64), far.long().expand((1 << 32) + 1)),
+                 lambda: batch.cache.read(far.long().expand((1 << 32) + 1))):
+        with pytest.raises(X.XenosError) as e:
+            call()
+        assert e.value.status == X.XENOS_EUNSUPPORTED, str(e.value)
+    want = T.attention(q, batch.cache, tables, lengths)
+    assert torch.equal(T.attention(q, batch.cache, tables, lengths, max_queries=(1 << 32) + 1), want)     # (no more queries than there are)

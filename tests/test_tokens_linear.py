@@ -284,3 +284,17 @@ def test_norm_of_rows_whose_squares_leave_the_range(cols, dtype):
             y = T.linear(x[:rows].cuda(), w, w_scale, gamma=gamma.cuda(), eps=eps)
             y_want, size = product_by_definition(q[:rows], want_scale[:rows].cuda(), w, w_scale, None, None, False)
             assert torch.all((y.double() - y_want).abs() <= (5.1 + cols / 256 + 36) * U32 * size + (U16 * y_want.abs() if dtype == torch.bfloat16 else 0) * 1.01 + 1e-38)
+
+
+@pytest.mark.gpu
+def test_sizes_that_pass_31_bits_are_refused():
+    """The C entries count in int: a size that does not fit is refused, not cut to its lower bits.  (Views of one element: nothing is allocated.)"""
+    w, w_scale = T.quantize_rows(drawn(16, 100, torch.float32, 2).cuda())
+    one = torch.zeros(1, 1, device="cuda")
+    for call in (lambda: T.linear(one.expand((1 << 32) + 1, 100), w, w_scale), lambda: T.quantize_rows(one.expand((1 << 32) + 1, 100)), lambda: T.quantize_rows(one.expand(1, (1 << 32) + 100)),
+                 lambda: T.linear(one.expand(1, (1 << 32) + 100), w, w_scale),
+                 lambda: T.quant_matmul(w[:1].expand((1 << 32) + 1, 128), one[0].expand((1 << 32) + 1), w, w_scale, 100),
+                 lambda: T.logprobs(one.expand(1, (1 << 32) + 5)), lambda: T.logprobs(one.expand((1 << 32) + 5, 7), top=2)):
+        with pytest.raises(X.XenosError) as e:
+            call()
+        assert e.value.status == X.XENOS_EUNSUPPORTED, str(e.value)
