@@ -144,7 +144,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, bias: Opt
         _check(residual, "residual", device, x.dtype, (*shape[:-1], out_c))
     if len(shape) != 2:
         x = x.reshape(-1, cols)
-        residual = None if residual is None else residual.reshape(-1, out_c)
+        residual = None if residual is None else residual.reshape(x.shape[0], out_c)
     x, residual, rows = _rows(x), None if residual is None else _rows(residual), x.shape[0]
     w_scale, bias, gamma = _given(w_scale, "w_scale", device, (out_c,)), _given(bias, "bias", device, (out_c,)), _given(gamma, "gamma", device, (cols,))
     out = x.new_empty((rows, out_c))

@@ -298,3 +298,13 @@ def test_sizes_that_pass_31_bits_are_refused():
         with pytest.raises(X.XenosError) as e:
             call()
         assert e.value.status == X.XENOS_EUNSUPPORTED, str(e.value)
+
+
+@pytest.mark.gpu
+def test_a_layer_without_outputs_takes_a_residual_of_any_dimensions():
+    w, w_scale = T.quantize_rows(drawn(5, 96, torch.float32, 2).cuda())
+    x = drawn(6, 96, torch.bfloat16, 1).cuda()
+    for shape in ((6, 96), (2, 3, 96), (6, 1, 1, 96)):
+        assert T.linear(x.view(shape), w[:0], w_scale[:0], residual=x.new_empty((*shape[:-1], 0))).shape == (*shape[:-1], 0)
+    assert T.linear(x[0], w[:0], w_scale[:0], residual=x.new_empty(0)).shape == (0,)
+    assert T.linear(x.view(2, 3, 96)[:, :0], w, w_scale, residual=x.new_empty(2, 0, 5)).shape == (2, 0, 5)
