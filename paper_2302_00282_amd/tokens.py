@@ -50,9 +50,14 @@ def _too_many(what: str):
     _refuse(X.XENOS_EUNSUPPORTED, f"{what}: sizes of at most {_INT_MAX}")
 
 
+def _needed(t: torch.Tensor, name: str, device: int, shape, dtype=torch.float32) -> torch.Tensor:
+    """A contiguous tensor of this shape and type."""
+    return _check(t, name, device, dtype, shape).contiguous()
+
+
 def _given(t: Optional[torch.Tensor], name: str, device: int, shape, dtype=torch.float32) -> Optional[torch.Tensor]:
-    """A contiguous tensor of this shape and type, or None."""
-    return None if t is None else _check(t, name, device, dtype, shape).contiguous()
+    """The same, or None."""
+    return None if t is None else _needed(t, name, device, shape, dtype)
 
 
 def _address(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -117,7 +122,7 @@ def quant_matmul(q: torch.Tensor, scale: torch.Tensor, w: torch.Tensor, w_scale:
         _too_many(f"q is {tuple(q.shape)}")
     q, w = q.contiguous(), _weights(w, device, cols)
     rows, out_c = q.shape[0], w.shape[0]
-    scale, w_scale, bias = _given(scale, "scale", device, (rows,)), _given(w_scale, "w_scale", device, (out_c,)), _given(bias, "bias", device, (out_c,))
+    scale, w_scale, bias = _needed(scale, "scale", device, (rows,)), _needed(w_scale, "w_scale", device, (out_c,)), _given(bias, "bias", device, (out_c,))
     if residual is not None:
         residual = _rows(_check(residual, "residual", device, dtype, (rows, out_c)))
     out = q.new_empty((rows, out_c), dtype=dtype)
@@ -146,7 +151,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, bias: Opt
         x = x.reshape(-1, cols)
         residual = None if residual is None else residual.reshape(x.shape[0], out_c)
     x, residual, rows = _rows(x), None if residual is None else _rows(residual), x.shape[0]
-    w_scale, bias, gamma = _given(w_scale, "w_scale", device, (out_c,)), _given(bias, "bias", device, (out_c,)), _given(gamma, "gamma", device, (cols,))
+    w_scale, bias, gamma = _needed(w_scale, "w_scale", device, (out_c,)), _given(bias, "bias", device, (out_c,)), _given(gamma, "gamma", device, (cols,))
     out = x.new_empty((rows, out_c))
     need = X.xenos_linear_workspace(rows, cols, out_c) if cols <= X.XENOS_QUANT_MAX_COLS else 0
     workspace = x.new_empty(need, dtype=torch.uint8) if need else None
@@ -199,7 +204,7 @@ class KVCache:
         if shape[0] > _INT_MAX:
             _too_many(f"k is {tuple(shape)}")
         _check(v, "v", self.device, k.dtype, shape)
-        slots = _given(slots, "slots", self.device, shape[:1], torch.int64)
+        slots = _needed(slots, "slots", self.device, shape[:1], torch.int64)
         if k.stride(2) != 1:
             k = k.contiguous()
         if v.stride(2) != 1:
@@ -246,8 +251,8 @@ def attention(q: torch.Tensor, cache: KVCache, tables: torch.Tensor, lengths: to
         max_length = ts[1] * cache.page_tokens
     if max(shape[0], shape[1], n_seqs, ts[1], max_length, prefix_length) > _INT_MAX:
         _too_many(f"{shape[0]} queries of {shape[1]} heads, tables of {tuple(ts)}, up to {max_length} tokens behind {prefix_length}")
-    tables = _given(tables, "tables", device, None, torch.int32)
-    lengths, starts = _given(lengths, "lengths", device, (n_seqs,), torch.int32), _given(starts, "starts", device, (n_seqs + 1,), torch.int32)
+    tables = _needed(tables, "tables", device, None, torch.int32)
+    lengths, starts = _needed(lengths, "lengths", device, (n_seqs,), torch.int32), _given(starts, "starts", device, (n_seqs + 1,), torch.int32)
     if starts is None and shape[0] != n_seqs:
         _refuse(X.XENOS_ESHAPE, f"{shape[0]} queries of {n_seqs} sequences, and no starts")
     prefix_table = _given(prefix_table, "prefix_table", device, None, torch.int32)

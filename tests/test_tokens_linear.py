@@ -308,3 +308,18 @@ def test_a_layer_without_outputs_takes_a_residual_of_any_dimensions():
         assert T.linear(x.view(shape), w[:0], w_scale[:0], residual=x.new_empty((*shape[:-1], 0))).shape == (*shape[:-1], 0)
     assert T.linear(x[0], w[:0], w_scale[:0], residual=x.new_empty(0)).shape == (0,)
     assert T.linear(x.view(2, 3, 96)[:, :0], w, w_scale, residual=x.new_empty(2, 0, 5)).shape == (2, 0, 5)
+
+
+@pytest.mark.gpu
+def test_tensors_that_are_not_given_are_refused():
+    w, w_scale = T.quantize_rows(drawn(16, 100, torch.float32, 2).cuda())
+    x = drawn(4, 100, torch.bfloat16, 1).cuda()
+    q, scale = T.quantize_rows(x)
+    cache = T.KVCache.empty(2, 16, 1, 16)
+    k, table, one = x.new_zeros(1, 1, 16), torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    for call in (lambda: T.linear(x, w, None), lambda: T.quant_matmul(q, None, w, w_scale, 100), lambda: T.quant_matmul(q, scale, w, None, 100), lambda: T.linear(x, None, w_scale),
+                 lambda: cache.write(k, k, None), lambda: cache.read(None), lambda: T.attention(k, cache, table, None)):
+        with pytest.raises(X.XenosError) as e:
+            call()
+        assert e.value.status == X.XENOS_EINVAL, str(e.value)
+    assert T.attention(k, cache, table, one - 1).shape == (1, 1, 16)
