@@ -41,9 +41,14 @@ def _check(t: torch.Tensor, name: str, device: Optional[int], dtype=None, shape=
         _refuse(X.XENOS_ESHAPE, f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
     if t.requires_grad and torch.is_grad_enabled():
         _refuse(X.XENOS_EUNSUPPORTED, f"{name} requires a gradient: these operators have no backward pass")
-    if _forward._current_level >= 0 and t.is_floating_point() and _forward.unpack_dual(t).tangent is not None:
-        _refuse(X.XENOS_EUNSUPPORTED, f"{name} has a tangent: these operators have no derivatives")
     return t
+
+
+def _no_tangents(*tensors: Optional[torch.Tensor]):
+    """Inside a level of forward-mode differentiation (asked once a call): no input has a tangent."""
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_floating_point() and _forward.unpack_dual(t).tangent is not None:
+            _refuse(X.XENOS_EUNSUPPORTED, f"an input {tuple(t.shape)} has a tangent: these operators have no derivatives")
 
 
 def _too_many(what: str):
@@ -57,7 +62,7 @@ def _needed(t: torch.Tensor, name: str, device: int, shape, dtype=torch.float32)
 
 def _given(t: Optional[torch.Tensor], name: str, device: int, shape, dtype=torch.float32) -> Optional[torch.Tensor]:
     """The same, or None."""
-    return None if t is None else _needed(t, name, device, shape, dtype)
+    return None if t is None else _check(t, name, device, dtype, shape).contiguous()
 
 
 def _address(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -96,6 +101,8 @@ def quantize_rows(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, eps: fl
     if rows > _INT_MAX or cols > _INT_MAX:
         _too_many(f"x is {rows} x {cols}")
     x, gamma = _rows(x), _given(gamma, "gamma", device, (cols,))
+    if _forward._current_level >= 0:
+        _no_tangents(x, gamma)
     q, scale = x.new_empty((rows, quant_pitch(cols)), dtype=torch.int8), x.new_empty(rows, dtype=torch.float32)
     _launch(device, X.xenos_quant_rows, x.data_ptr(), _DTYPE[x.dtype], rows, cols, x.stride(0), _address(gamma), eps, q.data_ptr(), scale.data_ptr())
     return q, scale
@@ -125,6 +132,8 @@ def quant_matmul(q: torch.Tensor, scale: torch.Tensor, w: torch.Tensor, w_scale:
     scale, w_scale, bias = _needed(scale, "scale", device, (rows,)), _needed(w_scale, "w_scale", device, (out_c,)), _given(bias, "bias", device, (out_c,))
     if residual is not None:
         residual = _rows(_check(residual, "residual", device, dtype, (rows, out_c)))
+    if _forward._current_level >= 0:
+        _no_tangents(scale, w_scale, bias, residual)
     out = q.new_empty((rows, out_c), dtype=dtype)
     args = X.QuantMatmulArgs(rows, cols, out_c, q.data_ptr(), scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), _address(bias), _address(residual),
                              0 if residual is None else residual.stride(0), relu, _DTYPE[dtype], out.data_ptr(), out_c)
@@ -152,6 +161,8 @@ def linear(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, *, bias: Opt
         residual = None if residual is None else residual.reshape(x.shape[0], out_c)
     x, residual, rows = _rows(x), None if residual is None else _rows(residual), x.shape[0]
     w_scale, bias, gamma = _needed(w_scale, "w_scale", device, (out_c,)), _given(bias, "bias", device, (out_c,)), _given(gamma, "gamma", device, (cols,))
+    if _forward._current_level >= 0:
+        _no_tangents(x, w_scale, bias, residual, gamma)
     out = x.new_empty((rows, out_c))
     need = X.xenos_linear_workspace(rows, cols, out_c) if cols <= X.XENOS_QUANT_MAX_COLS else 0
     workspace = x.new_empty(need, dtype=torch.uint8) if need else None
@@ -172,7 +183,7 @@ class KVCache:
         if k.dim() != 4:
             _refuse(X.XENOS_ESHAPE, f"k is {tuple(k.shape)}, not pages x heads x tokens x dimensions")
         n, heads, page, dim = k.shape
-        if max(k.shape) > _INT_MAX:
+        if n > _INT_MAX or heads > _INT_MAX or page > _INT_MAX:
             _too_many(f"k is {tuple(k.shape)}")
         _check(v, "v", device, torch.int8, (n, heads, page // 16, dim, 16))
         _check(k_scale, "k_scale", device, torch.float32, (n, heads, page))
@@ -181,6 +192,8 @@ class KVCache:
             _refuse(X.XENOS_EUNSUPPORTED, f"pages of {page} tokens, heads of {dim} values (multiples of 16, at most 256 values)")
         if not (k.is_contiguous() and v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()):
             _refuse(X.XENOS_ESHAPE, "the cache's tensors are not contiguous")
+        if _forward._current_level >= 0:
+            _no_tangents(k_scale, v_scale)
         self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, device
         self.n_pages, self.heads, self.page_tokens, self.head_dim = n, heads, page, dim
         self.desc = X.Cache(n, page, heads, dim, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
@@ -205,6 +218,8 @@ class KVCache:
             _too_many(f"k is {tuple(shape)}")
         _check(v, "v", self.device, k.dtype, shape)
         slots = _needed(slots, "slots", self.device, shape[:1], torch.int64)
+        if _forward._current_level >= 0:
+            _no_tangents(k, v)
         if k.stride(2) != 1:
             k = k.contiguous()
         if v.stride(2) != 1:
@@ -244,20 +259,23 @@ def attention(q: torch.Tensor, cache: KVCache, tables: torch.Tensor, lengths: to
         _refuse(X.XENOS_EUNSUPPORTED, f"q is {q.dtype}: bfloat16 is supported")
     if len(shape) != 3 or shape[2] != dim or shape[1] == 0 or shape[1] % cache.heads:
         _refuse(X.XENOS_ESHAPE, f"q is {tuple(shape)}, not queries x a multiple of {cache.heads} heads x {dim}")
+    n_queries, heads, _ = shape
     if len(ts) != 2:
         _refuse(X.XENOS_ESHAPE, f"tables is {tuple(ts)}, not sequences x pages")
-    n_seqs = ts[0]
+    n_seqs, pages = ts
     if max_length is None:
-        max_length = ts[1] * cache.page_tokens
-    if max(shape[0], shape[1], n_seqs, ts[1], max_length, prefix_length) > _INT_MAX:
-        _too_many(f"{shape[0]} queries of {shape[1]} heads, tables of {tuple(ts)}, up to {max_length} tokens behind {prefix_length}")
+        max_length = pages * cache.page_tokens
+    if n_queries > _INT_MAX or heads > _INT_MAX or n_seqs > _INT_MAX or pages > _INT_MAX or max_length > _INT_MAX or prefix_length > _INT_MAX:
+        _too_many(f"{n_queries} queries of {heads} heads, tables of {tuple(ts)}, up to {max_length} tokens behind {prefix_length}")
     tables = _needed(tables, "tables", device, None, torch.int32)
     lengths, starts = _needed(lengths, "lengths", device, (n_seqs,), torch.int32), _given(starts, "starts", device, (n_seqs + 1,), torch.int32)
-    if starts is None and shape[0] != n_seqs:
-        _refuse(X.XENOS_ESHAPE, f"{shape[0]} queries of {n_seqs} sequences, and no starts")
+    if starts is None and n_queries != n_seqs:
+        _refuse(X.XENOS_ESHAPE, f"{n_queries} queries of {n_seqs} sequences, and no starts")
     prefix_table = _given(prefix_table, "prefix_table", device, None, torch.int32)
     if prefix_length and not 0 < prefix_length <= (0 if prefix_table is None else prefix_table.numel() * cache.page_tokens):
         _refuse(X.XENOS_ESHAPE, f"a prefix of {prefix_length} tokens in {0 if prefix_table is None else prefix_table.numel()} pages of {cache.page_tokens}")
+    if _forward._current_level >= 0:
+        _no_tangents(q)
     if q.stride(2) != 1:
         q = q.contiguous()
     if out is None:
@@ -265,8 +283,8 @@ def attention(q: torch.Tensor, cache: KVCache, tables: torch.Tensor, lengths: to
     elif _check(out, "out", device, q.dtype, shape).stride(2) != 1:
         _refuse(X.XENOS_ESHAPE, "the rows of out are not contiguous")
     qs, os = q.stride(), out.stride()
-    args = X.AttentionArgs(n_seqs, shape[0], shape[1], X.XENOS_BF16, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1], _address(starts), lengths.data_ptr(),
-                           tables.data_ptr(), ts[1], min(max_queries, shape[0]), max_length, _address(prefix_table), prefix_length,
+    args = X.AttentionArgs(n_seqs, n_queries, heads, X.XENOS_BF16, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1], _address(starts), lengths.data_ptr(),
+                           tables.data_ptr(), pages, max_queries if max_queries < n_queries else n_queries, max_length, _address(prefix_table), prefix_length,
                            1.0 / math.sqrt(dim) if scale is None else scale)
     need = X.xenos_attention_workspace(cache.desc, args)
     workspace = q.new_empty(need, dtype=torch.uint8) if need else None
@@ -291,6 +309,8 @@ def logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: 
     if top > vocab:
         _refuse(X.XENOS_ESHAPE, f"the best {top} of {vocab} tokens")
     targets, logits = _given(targets, "targets", device, (rows,), torch.int64), _rows(logits)
+    if _forward._current_level >= 0:
+        _no_tangents(logits)
     given = None if targets is None else logits.new_empty(rows, dtype=torch.float32)
     entropy, best, token = logits.new_empty(rows, dtype=torch.float32), logits.new_empty((rows, top), dtype=torch.float32), logits.new_empty((rows, top), dtype=torch.int32)
     need = X.xenos_logprobs_workspace(rows, vocab, top)
