@@ -232,7 +232,7 @@ xenos_status xenos_probe_read(const xenos_hw_info* hw, const void* d_in, size_t 
  * the scale then also holds the row's factor 1 / sqrt(mean x^2 + eps).  A row that holds a NaN or an infinity stands for NaN.
  * The tokens' activations take this form on every call, a layer's weights ([out_c][cols], one scale per output channel) once.
  * x: `rows` rows of `cols` elements, row_stride elements apart.  q: rows XENOS_QUANT_PITCH(cols) bytes apart, zeros behind
- * the row's own values, 16-byte aligned.  cols is at most XENOS_QUANT_MAX_COLS (the sums of a product stay within 32 bits). */
+ * the row's own values, 16-byte aligned.  cols is at most XENOS_QUANT_MAX_COLS (the sums of a product stay within 32 bits), rows at most 2^30. */
 #define XENOS_QUANT_MAX_COLS 131072
 #define XENOS_QUANT_PITCH(cols) (((long long)(cols) + 127) / 128 * 128)
 xenos_status xenos_quant_rows(const void* d_x, xenos_dtype dtype, int rows, int cols, long long row_stride, const float* d_gamma, float eps,

@@ -25,6 +25,8 @@ xenos_status rows_of(const char* who, const void* d_x, xenos_dtype dtype, int ro
                      QuantRowsArgs& a) {
   if (rows < 0 || cols <= 0 || !known(dtype)) return fail(XENOS_EINVAL, "%s: %d rows of %d columns, type %d", who, rows, cols, (int)dtype);
   if (cols > XENOS_QUANT_MAX_COLS) return fail(XENOS_EUNSUPPORTED, "%s: %d columns, at most %d", who, cols, XENOS_QUANT_MAX_COLS);
+  // (a workgroup's row counter goes beyond the last row by less than the launch's workgroups)
+  if (rows > (1 << 30)) return fail(XENOS_EUNSUPPORTED, "%s: %d rows, at most %d", who, rows, 1 << 30);
   if (rows == 0) return XENOS_OK;
   if (!d_x || !d_q || !d_scale) return fail(XENOS_EINVAL, "%s: NULL argument", who);
   if (rows > 1 && row_stride < cols) return fail(XENOS_ESHAPE, "%s: rows of %d elements, %lld apart", who, cols, row_stride);

@@ -323,3 +323,16 @@ def test_tensors_that_are_not_given_are_refused():
             call()
         assert e.value.status == X.XENOS_EINVAL, str(e.value)
     assert T.attention(k, cache, table, one - 1).shape == (1, 1, 16)
+
+
+def test_more_rows_than_the_kernels_count_are_refused():
+    """A workgroup goes on by the grid's size behind the last row it had: a count within that of 2^31 would wrap."""
+    p = 256
+    for rows in ((1 << 30) + 1, (1 << 31) - 1):
+        with pytest.raises(X.XenosError) as e:
+            X.xenos_quant_rows(p, 1, rows, 1, 1, 0, 1e-5, p, p)
+        assert e.value.status == X.XENOS_EUNSUPPORTED
+        with pytest.raises(X.XenosError) as e:
+            X.xenos_linear(X.LinearArgs(rows=rows, cols=1, out_c=1, dtype=1, d_x=p, x_stride=1, d_gamma=None, eps=1e-5, d_w=p, d_w_scale=p, d_bias=None, d_residual=None, residual_stride=0,
+                                        relu=0, d_out=p, out_stride=1), p, 1 << 60)
+        assert e.value.status == X.XENOS_EUNSUPPORTED
