@@ -127,3 +127,54 @@ def test_a_captured_step_answers_as_an_eager_one(case):
         y = model.step(token)
         for a, b in zip((y, *T.logprobs(y, token, top=3)), replayed[i]):
             assert torch.equal(a, b)
+
+
+def room_of(device):
+    """A model with two sequences in pages for 16 tokens each, without its kernels: what it would ask of them is kept."""
+    model = M.TokenModel.__new__(M.TokenModel)
+    model.sizes, model.longest, model.room, model.prefix = SIZES, 16, 16, 0
+    model.tables, model.prefix_table = torch.tensor([[1], [2]], dtype=torch.int32, device=device), torch.zeros(1, dtype=torch.int32, device=device)
+    model.lengths, model.asked = torch.zeros(2, dtype=torch.int32, device=device), []
+    model._attend = lambda tokens, slots, starts, most: model.asked.append(slots.tolist())
+    return model
+
+
+def test_tokens_beyond_the_pages_are_refused_or_not_stored():
+    """On the CPU: an index beyond a table is an error there, and stops the whole process on a GPU."""
+    model = room_of("cpu")
+    model.append([torch.zeros(15, dtype=torch.int64), torch.zeros(3, dtype=torch.int64)])
+    model.step(torch.zeros(2, dtype=torch.int64))
+    assert model.asked == [[*range(16, 31), 32, 33, 34], [31, 35]]
+    for call in (lambda: model.append([torch.zeros(1, dtype=torch.int64)] * 2), lambda: model.append([torch.zeros(0, dtype=torch.int64)]),
+                 lambda: M.TokenModel.begin(model, torch.zeros(17, dtype=torch.int64))):
+        with pytest.raises(ValueError):
+            call()
+    assert model.lengths.tolist() == [16, 4] and len(model.asked) == 2
+    model.step(torch.zeros(2, dtype=torch.int64))
+    assert model.asked[-1] == [-1, 36] and model.lengths.tolist() == [17, 5]
+
+
+@pytest.mark.gpu
+def test_a_step_replayed_beyond_its_pages_leaves_the_others_alone(case):
+    weights, shared, own = case
+    model = M.TokenModel(SIZES, weights, 2, 16)
+    model.append([own[0], own[1]])                              # 9 and 1 of 16
+    token = torch.tensor([5, 6], device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        model.step(token)
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        logits = model.step(token)
+    replayed = []
+    for _ in range(10):                                         # lengths 20 and 12
+        graph.replay()
+        replayed.append(logits.clone())
+        torch.cuda.synchronize()
+    apart = M.TokenModel(SIZES, weights, 1, 16)
+    apart.append([own[1]])
+    apart.step(token[1:])
+    for y in replayed:
+        assert near(y[1:], apart.step(token[1:])) and torch.isfinite(y).all()

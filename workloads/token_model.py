@@ -64,7 +64,7 @@ class TokenModel:
         pages = torch.arange(front + n_seqs * own, dtype=torch.int32, device=device)
         self.prefix_table, self.tables = pages[:front], pages[front:].view(n_seqs, own)
         self.prefix, self.lengths = 0, torch.zeros(n_seqs, dtype=torch.int32, device=device)
-        self.longest = longest
+        self.longest, self.room = longest, own * s.page
 
     def _product(self, name: str, x: torch.Tensor, norm: Optional[str] = None, **kw) -> torch.Tensor:
         w, scale = self.layers8[name]
@@ -83,6 +83,8 @@ class TokenModel:
     def begin(self, tokens: torch.Tensor) -> torch.Tensor:
         """Takes the tokens (int64 [n]) that all sequences begin with; returns their logits."""
         n, page = len(tokens), self.sizes.page
+        if n > len(self.prefix_table) * page:
+            raise ValueError(f"{n} tokens in the {len(self.prefix_table)} pages of the shared beginning")
         at = torch.arange(n, device=tokens.device)
         slots = self.prefix_table.long()[at // page] * page + at % page
         table, length = self.prefix_table[None], torch.full((1,), n, dtype=torch.int32, device=tokens.device)
@@ -93,6 +95,9 @@ class TokenModel:
     def append(self, tokens: List[torch.Tensor]) -> torch.Tensor:
         """Takes some more tokens of each sequence (int64, any number of each); returns the logits of all, one sequence behind the other."""
         counts = [len(t) for t in tokens]
+        held = self.lengths.tolist()
+        if len(counts) != len(held) or max(a + b for a, b in zip(held, counts)) > self.room:
+            raise ValueError(f"{counts} more tokens of sequences of {held}, in pages for {self.room} each")
         device, page = self.lengths.device, self.sizes.page
         starts = torch.tensor([0, *torch.tensor(counts).cumsum(0).tolist()], dtype=torch.int32, device=device)
         seq = torch.repeat_interleave(torch.arange(len(counts), device=device), torch.tensor(counts, device=device))
@@ -101,9 +106,12 @@ class TokenModel:
         return self._attend(torch.cat(tokens), self.tables.long()[seq, at // page] * page + at % page, starts, max(counts))
 
     def step(self, tokens: torch.Tensor) -> torch.Tensor:
-        """Takes one more token of each sequence (int64 [sequences]); returns their logits.  No look at the device: a step can be captured in a graph."""
+        """Takes one more token of each sequence (int64 [sequences]); returns their logits.  No look at the device: a step can be captured in a graph.
+        Beyond the pages that a sequence has, nothing more of it is stored, and it is answered from what they hold."""
         at, page = self.lengths.long(), self.sizes.page
-        slots = self.tables.long().gather(1, (at // page)[:, None]).squeeze(1) * page + at % page
+        there = at < self.room
+        place = torch.where(there, at, torch.zeros_like(at))
+        slots = torch.where(there, self.tables.long().gather(1, (place // page)[:, None]).squeeze(1) * page + place % page, torch.full_like(at, -1))
         self.lengths += 1
         return self._attend(tokens, slots, None, 1)
 
