@@ -38,8 +38,13 @@ int quant_splits(int rows, int out_c, long long pitch);
 int launch_quant_matmul(const QuantMatmulArgs& a, int dtype, void* stream);
 // Both for one layer.  A few short rows are quantised by every workgroup of the product for itself, which saves a launch; r.q and r.scale are not used then.
 // (us in two launches, in one, among others in a graph: 1 x 512 x 2048: 5.5, 4.8; 1 x 4096 x 4096: 7.8, 6.2; 8 x 1024 x 4096: 7.0, 5.8; 16 x 512 x 2048: 6.0, 6.2; 8 x 2048 x 2048, beyond: 7.6, 7.1;
-// 16 x 1024 x 4096: 7.3, 7.6.  8192 bytes are also what the one turn of weights covers that is under way meanwhile.)
-inline bool linear_in_one(int rows, long long pitch) { return rows <= 16 && rows * pitch <= 8192; }
+// 16 x 1024 x 4096: 7.3, 7.6.  8192 bytes are also what the one turn of weights covers that is under way meanwhile.)  Each 16 outputs quantise the rows once more: where there
+// are 256 tiles of 64 outputs, which the product alone reads in tiles, that is worth it only beside the weights of one long row.  (In two launches, in one: 16 x 512 x 8192: 7.9, 8.7;
+// x 16384: 8.1, 15.3; x 131072: 30, 108; 4 x 2048 x 16320: 17.9, 16.5; x 16384: 11.6, 16.5; 1 x 2048 x 32000: 18, 27; 2 x 4096 x 32000: 33, 37; 1 x 4096 x 16384: 20.4, 19.5;
+// x 32000: 31.8, 33.5; x 131072: 139, 121; 1 x 8192 x 65536: 134, 100.)
+inline bool linear_in_one(int rows, long long pitch, int out_c) {
+  return rows <= 16 && rows * pitch <= 8192 && (out_c <= 255 * 64 || (rows == 1 && pitch >= 4096));
+}
 int launch_linear(const QuantRowsArgs& r, const QuantMatmulArgs& a, int dtype, void* stream);
 
 struct CacheArgs {

@@ -522,7 +522,7 @@ int launch_quant_matmul(const QuantMatmulArgs& a, int dtype, void* stream) {
 }
 
 int launch_linear(const QuantRowsArgs& r, const QuantMatmulArgs& a, int dtype, void* stream) {
-  if (linear_in_one(a.M, a.pitch)) {
+  if (linear_in_one(a.M, a.pitch, a.N)) {
     const int nt = (a.N + 15) / 16, lds = a.M * (int)a.pitch;
     if (dtype) quant_matvec_kernel<bf16_t, 1, true><<<nt, 512, lds, (hipStream_t)stream>>>(a, r);
     else quant_matvec_kernel<float, 1, true><<<nt, 512, lds, (hipStream_t)stream>>>(a, r);

@@ -65,7 +65,7 @@ struct LinearSpace {
 LinearSpace linear_space(int rows, int cols, int out_c) {
   const long long pitch = quant_pitch(cols);
   LinearSpace s{};
-  if (rows == 0 || linear_in_one(rows, pitch)) return s;
+  if (rows == 0 || linear_in_one(rows, pitch, out_c)) return s;
   s.scale = (size_t)rows * pitch;
   s.part = (s.scale + (size_t)rows * 4 + 15) / 16 * 16;
   s.splits = quant_splits(rows, out_c, pitch);

@@ -336,3 +336,23 @@ def test_more_rows_than_the_kernels_count_are_refused():
             X.xenos_linear(X.LinearArgs(rows=rows, cols=1, out_c=1, dtype=1, d_x=p, x_stride=1, d_gamma=None, eps=1e-5, d_w=p, d_w_scale=p, d_bias=None, d_residual=None, residual_stride=0,
                                         relu=0, d_out=p, out_stride=1), p, 1 << 60)
         assert e.value.status == X.XENOS_EUNSUPPORTED
+
+
+def test_wide_outputs_of_short_rows_take_two_launches():
+    """(Their rows then lie in the workspace.)"""
+    for rows, cols, out_c, one in [(1, 512, 2048, True), (16, 512, 255 * 64, True), (16, 512, 255 * 64 + 1, False), (16, 512, 32000, False), (1, 2048, 32000, False), (2, 4096, 32000, False),
+                                   (1, 4096, 32000, True), (1, 8192, 131072, True), (1, 8193, 16, False), (17, 128, 16, False)]:
+        assert (X.xenos_linear_workspace(rows, cols, out_c) == 0) == one
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols,out_c", [(16, 512, 16320), (16, 500, 16321), (1, 4000, 16400), (2, 4096, 16500), (1, 100, 33000)])
+def test_wide_outputs_of_short_rows(rows, cols, out_c, dtype):
+    x = drawn(rows, cols, dtype, 1).cuda()
+    w, w_scale = T.quantize_rows(drawn(out_c, cols, torch.float32, 2).cuda())
+    q, scale = T.quantize_rows(x)
+    bias = drawn(1, out_c, torch.float32, 5)[0].cuda()
+    assert torch.equal(T.linear(x, w, w_scale, bias=bias), T.quant_matmul(q, scale, w, w_scale, cols, dtype=dtype, bias=bias))
+    want, size = product_by_definition(q, scale, w, w_scale, bias, None, False)
+    assert torch.all((T.linear(x, w, w_scale, bias=bias).double() - want).abs() <= 5.1 * U32 * size + (U16 * want.abs() if dtype == torch.bfloat16 else 0) + 1e-38)
