@@ -11,7 +11,7 @@ namespace xenos {
 namespace {
 
 constexpr float kLowest = -3.402823466e38f, kLog2e = 1.44269504088896340736f;
-constexpr float kSlack = 8.f;                                 // a maximum is followed when it has grown by more: terms up to e^8 are as exact
+constexpr float kSlack = 1.f;                                 // a maximum is followed when it has grown by more (the exponents' own rounding goes with their size: 8 was no faster)
 constexpr int kPer = 16, kBlock = 64 * kPer;                  // elements per lane and wavefront at a time
 
 // (bits of v in their order, ties to the lower index); NaN above all, -0 as 0
@@ -177,8 +177,10 @@ __global__ __launch_bounds__(256, 8) void logprobs_kernel(LogprobsArgs a) {
     for (int e = 1; e + 1 < kPer; e += 2) top = max3_raw(top, f[e], f[e + 1]);
     top = fmx_raw(top, f[kPer - 1]);
     if (__any(top > z.m + kSlack)) z.raise(fmaxf(z.m, top));
+    Sums here{z.m, 0.f, 0.f};                                 // (by itself: terms added one by one to all that went before would be lost behind a few large ones)
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) z.add(f[e]);
+    for (int e = 0; e < kPer; ++e) here.add(f[e]);
+    z.s += here.s, z.t += here.t;
     if (!TOP) continue;
     const int i0 = begin - shift + b;                         // (of lane 0)
     // What equals the last one comes after it, since its index is higher than any seen in an earlier block.  The first block has no last one: the top-th of the lanes' largest

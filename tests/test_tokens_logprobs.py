@@ -202,3 +202,39 @@ def test_masked_and_steep_rows_have_numbers_too(vocab, dtype):
     check_strictly(x, targets, 20)
     targets = torch.tensor([1, 5, 0, vocab - 1, 0, 0, 1, 101, 0, 1], device="cuda")
     check_strictly(x, targets, 3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("large", [64, 4096])
+def test_many_small_terms_behind_large_ones_are_not_lost(large, dtype):
+    """Each term is less than half a step of what its lane has summed by then; together they are what the bound sees.  (So many rows that none is cut in parts.)"""
+    vocab, rows = 200000, 1030
+    x = torch.full((rows, vocab), -13.9375, dtype=dtype, device="cuda")         # e^x = 8.9e-7
+    x[:, :large] = 0
+    targets = torch.full((rows,), vocab - 1, device="cuda")
+    given, entropy, best, token = T.logprobs(x, targets, 2)
+    total = large + (vocab - large) * math.exp(-13.9375)
+    # sums of 16 terms, of a wavefront's blocks, of the lanes and wavefronts; an exponential's two steps; the differences and the logarithm of size 14 and 9
+    bound = (16 + vocab / 4096 + 12 + 4) * U32 + (14 + 9) * U32
+    assert (given.double() + 13.9375 + math.log(total)).abs().max() <= bound
+    assert (best.double() + math.log(total)).abs().max() <= bound
+    want = math.log(total) + (vocab - large) * math.exp(-13.9375) * 13.9375 / total
+    assert (entropy.double() - want).abs().max() <= 3 * bound
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_entropies_are_as_near_as_their_sums(dtype):
+    """Rows whose largest logit comes late and is little above the first block's: what was summed before it counts in its steps."""
+    rows, vocab = 1030, 20000
+    x = drawn(rows, vocab, dtype, 3, 2.5)
+    x[:, 15000] = x[:, :4096].amax(-1) + 7.5
+    given, entropy, best, token = T.logprobs(x, torch.full((rows,), 15000, device="cuda"), 1)
+    want, want_entropy, lp = by_definition(x[:64], torch.full((64,), 15000))
+    d = (lp - lp.amax(-1, keepdim=True)).abs()
+    weighed = (lp.exp() * d).sum(-1)                            # (of an exponent: a step of its size and two of its exponential)
+    sums = (16 + vocab / 4096 + 12 + 4) * U32 + 2 * U32 * weighed
+    assert torch.all((given[:64].double().cpu() - want).abs() <= sums + 24 * U32 + 2 * U32 * want.abs())
+    second = (lp.exp() * d * d).sum(-1)
+    assert torch.all((entropy[:64].double().cpu() - want_entropy).abs() <= 2 * sums * (1 + weighed) + 2 * U32 * second + 24 * U32)
