@@ -240,7 +240,8 @@ xenos_status xenos_quant_rows(const void* d_x, xenos_dtype dtype, int rows, int 
 
 /* Product of two such matrices: out[m][n] = act(scale[m] * w_scale[n] * sum_k q[m][k] w[n][k] + bias[n] + residual[m][n]).
  * The sum is a whole number, exact; the rest is fp32, rounded once to `dtype`.  q and w: XENOS_QUANT_PITCH(cols) bytes a row, 16-byte aligned, zeros behind
- * column `cols`; weights lie in -127 .. 127.  residual (of `dtype`, may be NULL; may be out itself) and bias (may be NULL) as in the linked chains: added before the ReLU. */
+ * column `cols`; weights lie in -127 .. 127.  residual (of `dtype`, may be NULL; may be out itself) and bias (may be NULL) as in the linked chains: added before the ReLU.
+ * There is no workspace, so K is never made in shares: few rows of many columns take longer than inside xenos_linear (32 x 25088 x 4096: 35 us, there 26). */
 typedef struct {
   int rows, cols, out_c;
   const void* d_q;

@@ -142,7 +142,7 @@ constexpr float kHead = 7.f, kSlack = 15.f, kLeastScale = 0x1p-88f;
 __device__ __forceinline__ float size_of_scale(float s) { return __builtin_amdgcn_logf(fmaxf(fabsf(s), kLeastScale)); }
 
 // Few rows: the wavefronts of a workgroup have the same 16 rows and take turns with the keys; their states meet in LDS at the end.  NB: blocks of 64 dimensions.
-// Bound by the cache's bytes: 16 sequences of 100 to 32768 tokens, 8 heads of 128, 32 of queries: 506 MB in 100 to 109 us, 4.6 to 5 TB/s; all of 32768: 1.1 GB in 206, 5.4 TB/s.
+// Bound by the cache's bytes: 16 sequences of 100 to 32768 tokens, 8 heads of 128, 32 of queries: 506 MB in 100 to 112 us, 4.5 to 5 TB/s; all of 32768: 1.1 GB in 206, 5.4 TB/s.
 template <int NB>
 __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_kernel(AttentionArgs a) {
   constexpr int DT = 4 * NB, REC = 4 * DT + 2;              // tiles of 16 dimensions; floats of a lane's state
@@ -339,8 +339,8 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 4 - NB : 1) void attention_k
 // Many rows: the four wavefronts of a workgroup have 32 rows each and pass over the same keys, which the workgroup turns into bf16 and fp16 once, in LDS, while the steps before
 // them are multiplied.  S^T = K Q^T in blocks of 32 keys x 32 rows, whose row 8 a + 4 h + b is key 16 (a / 2) + 8 h + 4 (a % 2) + b: a lane of half h then holds eight
 // neighbouring keys at a time, an operand of O^T += V^T P^T as it is.
-// Bound by the vector instructions beside the products (the softmax's, a dozen a score, and the conversions): a prompt of 4097, 20 heads of 128 on 4: 86 GFLOP in 143 to 166 us, 520 to 600 TFLOP/s;
-// 512 rows to 16384 shared keys on 4 heads of 128: 17 GFLOP in 37 us.
+// Bound by the vector instructions beside the products (the softmax's, a dozen a score, and the conversions): a prompt of 4097, 20 heads of 128 on 4: 86 GFLOP in 144 to 168 us, 510 to 600 TFLOP/s;
+// 512 rows to 16384 shared keys on 4 heads of 128: 17 GFLOP in 39 us.
 // Whether a weight may pass 2^kSlack is judged by the largest scale of a step, whoever sees it; only if it may are the scales of the keys that a row sees looked at one by one.
 template <int NB>
 __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_kernel(AttentionArgs a) {
@@ -582,7 +582,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void attention_tile_k
 }
 
 // The pieces of a row put together by a workgroup: every wavefront weighs them all, then groups of dim / 4 lanes add four dimensions each of several pieces at a time.
-// Bound by their bytes: 2048 rows of 128 in 33 pieces: 35 MB in 8.3 us, 4.2 TB/s.
+// Bound by their bytes: 2048 rows of 128 in 33 pieces: 35 MB in 8.5 us, 4.1 TB/s.
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
   __shared__ float s_w[2 * kMostParts];
   __shared__ f32x4_t s_o[256];
@@ -668,11 +668,11 @@ int attention(AttentionArgs a, hipStream_t st) {
 }
 
 // Which kernel a segment has.  More than 32 rows, and rows x keys x dimensions of 1.6e9 at the least: many rows; below, its few workgroups and its way into LDS cost more than it saves.
-// us for 16 rows a workgroup, for many rows (8 heads of 128, keys x sequences x rows): 8192 x 1 x 128: 26, 30; 5869 x 1 x 128 (dim 64): 18, 26; 8192 x 4 x 64: 40, 36; 8192 x 1 x 512: 65,
-// 45; 2048 x 8 x 1024: 200, 94; 4 heads, 4097 x 1 x 20485, each row up to its own: 264, 143.
+// us for 16 rows a workgroup, for many rows (8 heads of 128, keys x sequences x rows): 8192 x 1 x 128: 33, 36; 5869 x 1 x 128 (dim 64): 17, 21; 8192 x 4 x 64: 54, 39; 8192 x 1 x 512: 79,
+// 49; 2048 x 8 x 1024: 176, 99; 4 heads, 4097 x 1 x 20485, each row up to its own: 264, 147.
 // The keys are cut in pieces until there are `want` workgroups, none shorter than two steps of every wavefront that takes turns with it: 16 rows, heads up to 128, 2048 (16 sequences of 100 to
-// 32768 tokens, 8 heads of 128: in 512 130 us, in 2048 110; where all have 32768, 198 and 206); longer heads, of which a unit holds a workgroup or two, and many rows: 512 (32 sequences of 4042,
-// 16 heads of 256: 126 us, in 2048 157; 8 sequences of 2048 with 1024 rows: 94, in 1024 166).
+// 32768 tokens, 8 heads of 128: in 512 140 us, in 2048 122; where all have 32768, 203 and 210); longer heads, of which a unit holds a workgroup or two, and many rows: 512 (32 sequences of 4042,
+// 16 heads of 256: 190 us, in 2048 235; 8 sequences of 2048 with 1024 rows: 98, in 1024 175).
 void share_out(AttentionShare& s, int dim, long long rows, long long times, long long tokens) {
   s.many = rows > 32 && (double)(rows * times) * (double)tokens * dim >= 1.6e9;
   const long long tile = s.many ? 32 * kWaves : 16, step = kKeys * (s.many ? 1 : kWaves), want = s.many || dim > 128 ? 512 : 2048;

@@ -150,7 +150,7 @@ __device__ __forceinline__ void join_waves(const LogprobsArgs& a, Sums z, uint64
 }
 
 // A workgroup per part of a row; its wavefronts take blocks of the part in turn.  Bound by vector instructions, some 25 places of issue an element (an exponential is four of them): 2048 x 100003 in bf16 with
-// the best tokens takes 140 to 150 us, 2.8 TB/s; 1 x 32000 10 us (in 7 parts of four or more blocks, whose first fill the lists).
+// the best tokens takes 127 to 145 us, 2.8 to 3.2 TB/s; 1 x 32000 10 us (in 7 parts of four or more blocks, whose first fill the lists).
 template <typename T, bool TOP>
 __global__ __launch_bounds__(256, 8) void logprobs_kernel(LogprobsArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = (int)blockIdx.x / a.parts, part = (int)blockIdx.x - row * a.parts;
@@ -252,8 +252,8 @@ int logprobs(const LogprobsArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Rows are read whole where there are enough of them to fill the units, else in up to 64 parts of at least four blocks, 1024 workgroups in all.  us whole, in parts (bf16, the five best): 1 x 32000: 17, 14.5;
-// 1 x 151936: 45, 17; 64 x 100003: 36, 20 (of 256 workgroups: 23); 512 x 100003: 54, 45; 256 x 32000: 20, 20; 1024 x 32000, in two: 30, 35.
+// Rows are read whole where there are enough of them to fill the units, else in up to 64 parts of at least four blocks, 1024 workgroups in all.  us whole, in parts (bf16, the five best): 1 x 32000: 17, 15;
+// 1 x 151936: 43, 16.5; 64 x 100003: 34, 21 (of 256 workgroups: 23); 512 x 100003: 50, 45; 256 x 32000: 20, 20; 1024 x 32000, in two: 30, 36.
 void logprobs_split(int rows, int vocab, int* parts, int* part_len) {
   const long long want = std::max(1, std::min(64, 1024 / std::max(1, rows))), most = std::max(1, vocab / (4 * kBlock));
   const int len = (int)((vocab + std::min(want, most) - 1) / std::min(want, most));

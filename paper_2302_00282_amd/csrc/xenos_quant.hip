@@ -272,7 +272,7 @@ __device__ __forceinline__ void quant_into_lds(const QuantRowsArgs& a, int8_t* q
 // Few rows: the weights are the work.  A workgroup has 16 output channels and all of K, which its wavefronts share; every fragment of the weights goes
 // from memory to registers, a lane's 16 bytes of one weight row at a time, and the sums (whole numbers: exact in any order) meet in LDS.
 // Bound by the weights' bytes where there are many (1 x 25088 x 4096: 17.7 us, 5.8 TB/s), by its chain of trips to memory and LDS where there are few.
-// OWN: x comes as it is, and every workgroup quantises all of it for itself (1 x 512 x 2048 in one launch: 5.8 us; linear_in_one).
+// OWN: x comes as it is, and every workgroup quantises all of it for itself (1 x 512 x 2048 in one launch: 5.9 us; linear_in_one).
 template <typename T, int MT, bool OWN>
 __global__ __launch_bounds__(512) void quant_matvec_kernel(QuantMatmulArgs a, QuantRowsArgs qa) {
   __shared__ i32x4_t part[8][MT][64];

@@ -20,3 +20,10 @@ def test_no_vector_register_is_spilled(kernels, kernel):  # noqa: F811
 def test_units_hold_the_wavefronts_that_were_planned(kernels, kernel, most):  # noqa: F811
     found = {k: v for k, v in kernels.items() if re.search(r"\d" + kernel, k)}
     assert found and not {k: v["vgpr_count"] for k, v in found.items() if v["vgpr_count"] > most}
+
+
+@pytest.mark.parametrize("kernel,most", [("logprobs_kernelI\\w+Lb1E", 4), ("attention_kernelILi4E", 6), ("attention_tile_kernelILi4E", 21)])
+def test_few_registers_are_spilled_where_some_are(kernels, kernel, most):  # noqa: F811
+    """Best tokens at eight wavefronts a unit, and heads beyond 192: what they spill is known, and small."""
+    found = {k: v for k, v in kernels.items() if re.search(r"\d" + kernel, k)}
+    assert found and not {k: v["vgpr_spill_count"] for k, v in found.items() if v["vgpr_spill_count"] > most}
